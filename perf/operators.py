@@ -219,7 +219,7 @@ def prepare(case, seed):
         # from flat rows to sure ones: a few tokens raised, some never allowed
         x = torch.randn(M, V, generator=g, **dev) * 2.0
         top = torch.randint(0, V, (M, 8), generator=g, **dev)
-        x.scatter_add_(1, top, 12.0 * torch.rand(M, 8, generator=g, **dev))
+        x.scatter_add_(1, top, 24.0 * torch.rand(M, 1, generator=g, **dev) * torch.rand(M, 8, generator=g, **dev))
         x[:, V - 1 - V // 50:] = -torch.inf
         s["x"] = x.to(getattr(torch, c["dtype"]))
         s["u"] = torch.rand(M, generator=g, **dev)
