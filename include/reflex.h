@@ -392,6 +392,146 @@ int reflex_moe_forward_noalloc(const reflex_moe_args* args, void* stream);
 int reflex_moe_forward_timed(const reflex_moe_args* args, void* ws, size_t ws_bytes, void* stream,
                              void* const* stage_events, int n_stage_events);
 
+/* ---- 8-bit products --------------------------------------------------------------
+ * Matrices of 8-bit floating point numbers (e4m3: 3 fraction bits, largest 448, no
+ * infinities, NaN 0x7f) with one scale for each block of 128 columns.  A block's scale
+ * is a power of two, held as the byte e of 2^(e - 127): the smallest for which the
+ * block's largest magnitude is at most 448 scales (1 .. 247; 127 for a block of
+ * zeros).  A code is the number over its scale, rounded to nearest with ties to even.
+ * A number that is not finite becomes NaN and takes no part in its block's scale.
+ *
+ *  rows     codes [M, K] row-major; every row has its own scale per 128 columns, the
+ *           scale of columns 128 b .. of row i at [b / 4][i][b % 4] of a byte array
+ *           [ceil(K / 512), M, 4] (reflex_fp8_scale_bytes(M, K) bytes);
+ *  weights  codes [N, K] row-major; one scale per 128 x 128 block, that of rows 128 a ..
+ *           and columns 128 b .. at [a][b] of a byte array [ceil(N / 128), 4 ceil(K / 512)]
+ *           (reflex_fp8_weight_scale_bytes(N, K) bytes, experts one after the other).
+ * Bytes for blocks past K are padding: the quantisers write 0, nothing reads them.
+ * K is a multiple of 128 and at most REFLEX_MAX_DIM; M and N are any.  Codes must be
+ * 16-byte aligned, scale arrays 4-byte aligned. */
+#define REFLEX_FP8_BLOCK 128
+size_t reflex_fp8_scale_bytes(int M, int K);           /* 0 on invalid sizes */
+size_t reflex_fp8_weight_scale_bytes(int N, int K);
+
+/* Element types of the operands that come in several. */
+#define REFLEX_TYPE_BF16 0
+#define REFLEX_TYPE_F32  1
+
+/*
+ * The masked positions (Section 3.1) as a list: rows[0 .. n-1] are the indices i with
+ * masked[i] != 0, ascending, n_rows[0] = n.  A head that predicts only those rows reads
+ * the list and the count on the device (reflex_quantize_fp8, reflex_matmul_fp8,
+ * reflex_sample_tokens).
+ *  masked [T] uint8;  rows [T] int32 output, entries from n on untouched;  n_rows [1]
+ *  int32 output (0 for T = 0);  ws >= reflex_select_rows_workspace_size(T) bytes
+ * Errors: NULL pointers; T out of range; workspace too small.
+ */
+size_t reflex_select_rows_workspace_size(int T);
+int reflex_select_rows(const uint8_t* masked, int T, int32_t* rows, int32_t* n_rows, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/*
+ * bf16 rows to 8-bit rows.  Row j of the output is row rows[j] of x (rows NULL: row j);
+ * rows from n_rows[0] on (n_rows NULL: M) are left as they were, a source row outside
+ * [0, x_rows) gives a row of zeros.
+ *  x [x_rows, K] bf16;  rows [M] int32 or NULL (then x_rows >= M);  n_rows [1] int32 on
+ *  the device or NULL;  q [M, K] codes;  scale [ceil(K / 512), M, 4]
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE); rows NULL with x_rows < M.
+ */
+int reflex_quantize_fp8(const uint16_t* x, const int32_t* rows, const int32_t* n_rows, int x_rows,
+                        int M, int K, uint8_t* q, uint8_t* scale, void* stream);
+
+/*
+ * bf16 weights of E experts (1: a plain matrix) to 8-bit weights.
+ *  w [E, N, K] bf16;  q [E, N, K] codes;  scale [E, ceil(N / 128), 4 ceil(K / 512)]
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE; E up to REFLEX_MAX_EXPERTS).
+ */
+int reflex_quantize_fp8_weight(const uint16_t* w, int E, int N, int K, uint8_t* q, uint8_t* scale,
+                               void* stream);
+
+/*
+ * out[i, n] = sum_k x[i, k] w[n, k] of 8-bit rows and weights, accumulated in fp32 on the
+ * matrix cores and rounded once (out_type REFLEX_TYPE_BF16) or stored as it is
+ * (REFLEX_TYPE_F32).  Rows from n_rows[0] on (n_rows NULL: M) are left as they were.
+ *  x [M, K], x_scale;  w [N, K], w_scale;  out [M, N] dense (16-byte aligned)
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE); unknown out_type (REFLEX_ERR_PARAM).
+ */
+int reflex_matmul_fp8(const uint8_t* x, const uint8_t* x_scale, const uint8_t* w,
+                      const uint8_t* w_scale, const int32_t* n_rows, int M, int N, int K,
+                      int out_type, void* out, void* stream);
+
+/*
+ * reflex_grouped_swiglu on 8-bit rows and weights.  For row j of expert e, x the row
+ * sorted_token[j] of h:  g = W_gate[e] x, u = W_up[e] x and SiLU(g) * u in fp32, rounded
+ * to an 8-bit row (as reflex_quantize_fp8 does, from fp32), y_sorted[j] = W_down[e] of
+ * it, accumulated in fp32 and rounded to bf16 once.
+ *  h [T, d], h_scale;  w_gate, w_up [E, f, d], w_down [E, d, f] with s_gate, s_up, s_down;
+ *  sorted_token, expert_offsets, pair_capacity, y_sorted as in reflex_grouped_swiglu
+ *  ws  scratch of >= reflex_swiglu_fp8_workspace_size(pair_capacity, E, f)
+ * Errors: NULL pointers; d % 128 or f % 128 nonzero; workspace too small.
+ */
+size_t reflex_swiglu_fp8_workspace_size(int pair_capacity, int E, int f);
+int reflex_grouped_swiglu_fp8(const uint8_t* h, const uint8_t* h_scale, const int32_t* sorted_token,
+                              const int32_t* expert_offsets, const uint8_t* w_gate,
+                              const uint8_t* w_up, const uint8_t* w_down, const uint8_t* s_gate,
+                              const uint8_t* s_up, const uint8_t* s_down, int T, int E, int d,
+                              int f, int32_t pair_capacity, uint16_t* y_sorted, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/*
+ * reflex_moe_forward with the routed and the shared experts in 8 bits: the router, the
+ * counts, TopK and the combine as there (from the bf16 h), the experts as
+ * reflex_grouped_swiglu_fp8 on h quantised by the call.  The expert weights of `args`
+ * (w_gate .. ws_down) are not read and may be NULL.
+ *  ws: >= reflex_workspace_fp8_size(T, E, d, f, f_shared, kcap) bytes, 256-byte aligned
+ * Errors: as reflex_moe_forward; f or f_shared not a multiple of 128 (REFLEX_ERR_SHAPE).
+ */
+typedef struct {
+  const uint8_t *w_gate, *w_up, *w_down;      /* codes [E, f, d], [E, f, d], [E, d, f]          */
+  const uint8_t *s_gate, *s_up, *s_down;      /* their scales                                   */
+  const uint8_t *ws_gate, *ws_up, *ws_down;   /* shared [fs, d], [fs, d], [d, fs] (f_shared > 0) */
+  const uint8_t *ss_gate, *ss_up, *ss_down;
+} reflex_fp8_experts;
+size_t reflex_sizeof_fp8_experts(void);       /* sizeof(reflex_fp8_experts)                     */
+size_t reflex_workspace_fp8_size(int T, int E, int d, int f, int f_shared, int k_max);
+int reflex_moe_forward_fp8(const reflex_moe_args* args, const reflex_fp8_experts* experts, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* ---- tokens and confidences ----------------------------------------------------------
+ * The token a forward predicts at each position and its confidence c^t (Section 3.1), as
+ * reflex_advance_state takes it, from rows of logits and given uniform numbers.
+ * Row j of the logits is position i = rows[j] (rows NULL: i = j), j < n_rows[0] (n_rows
+ * NULL: M); positions outside [0, T) are skipped, those of no row are left as they were.
+ *   weight of token v:  w_v = exp((l_v - max l) / temperature), in fp64
+ *   kept tokens, in the order (logit descending, index ascending, -0.0 == +0.0): the first
+ *     top_k; of those the shortest prefix whose weights sum to at least top_p of theirs;
+ *     of those the ones with w_v >= min_p.  The first token is always kept.
+ *   tokens[i] = the first kept v by index for which the kept weights up to v sum to more
+ *     than u[i] of the kept weights' sum; temperature 0: the first token of the order.
+ *   conf[i] = the softmax of the row's logits (temperature 1, all tokens) at tokens[i].
+ * A logit of -inf has weight 0 and so has NaN; where some are +inf they alone have
+ * weight, the same each.  A row without any weight gives token -1, confidence 0.
+ *  logits [M, V], logits_type REFLEX_TYPE_*;  u [T] fp32 in [0, 1) (others are clamped);
+ *  tokens [T] int32, conf [T] fp32 outputs (conf NULL: skipped)
+ *  ws >= reflex_sample_workspace_size(M, V) bytes (NULL where that is 0)
+ * params (host):  temperature >= 0 and finite; top_k >= 0 (0: all); 0 < top_p <= 1;
+ *  0 <= min_p <= 1 (REFLEX_ERR_PARAM otherwise).
+ * Errors: NULL pointers; sizes; unknown logits_type; workspace too small.
+ */
+typedef struct {
+  float   temperature;
+  int32_t top_k;
+  float   top_p;
+  float   min_p;
+} reflex_sample_params;
+#define REFLEX_MAX_VOCAB (1 << 20)     /* V <= this                                      */
+size_t reflex_sizeof_sample_params(void);
+size_t reflex_sample_workspace_size(int M, int V);
+int reflex_sample_tokens(const void* logits, int logits_type, const int32_t* rows,
+                         const int32_t* n_rows, int M, int V, const float* u,
+                         const reflex_sample_params* params, int T, int32_t* tokens, float* conf,
+                         void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -43,6 +43,18 @@ class MoeArgsC(ctypes.Structure):
                 + [(n, c_void_p) for n in _OUT_PTRS])
 
 
+class Fp8ExpertsC(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("w_gate", "w_up", "w_down", "s_gate", "s_up", "s_down",
+                                        "ws_gate", "ws_up", "ws_down", "ss_gate", "ss_up",
+                                        "ss_down")]
+
+
+class SampleParamsC(ctypes.Structure):
+    """temperature, top_k (0: all), top_p (1: all), min_p (0: all)."""
+    _fields_ = [("temperature", c_float), ("top_k", c_int32), ("top_p", c_float),
+                ("min_p", c_float)]
+
+
 _SIGS = {
     "reflex_version": (c_int, []),
     "reflex_status_string": (ctypes.c_char_p, [c_int]),
@@ -71,6 +83,26 @@ _SIGS = {
     "reflex_moe_forward_timed": (c_int, [ctypes.POINTER(MoeArgsC), c_void_p, c_size_t, c_void_p,
                                          ctypes.POINTER(c_void_p), c_int]),
     "reflex_moe_forward_noalloc": (c_int, [ctypes.POINTER(MoeArgsC), c_void_p]),
+    "reflex_fp8_scale_bytes": (c_size_t, [c_int, c_int]),
+    "reflex_fp8_weight_scale_bytes": (c_size_t, [c_int, c_int]),
+    "reflex_select_rows_workspace_size": (c_size_t, [c_int]),
+    "reflex_select_rows": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_size_t,
+                                   c_void_p]),
+    "reflex_quantize_fp8": (c_int, [c_void_p] * 3 + [c_int] * 3 + [c_void_p] * 3),
+    "reflex_quantize_fp8_weight": (c_int, [c_void_p] + [c_int] * 3 + [c_void_p] * 3),
+    "reflex_matmul_fp8": (c_int, [c_void_p] * 5 + [c_int] * 4 + [c_void_p] * 2),
+    "reflex_swiglu_fp8_workspace_size": (c_size_t, [c_int, c_int, c_int]),
+    "reflex_grouped_swiglu_fp8": (c_int, [c_void_p] * 10 + [c_int] * 4
+                                  + [c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "reflex_sizeof_fp8_experts": (c_size_t, []),
+    "reflex_workspace_fp8_size": (c_size_t, [c_int] * 6),
+    "reflex_moe_forward_fp8": (c_int, [ctypes.POINTER(MoeArgsC), ctypes.POINTER(Fp8ExpertsC),
+                                       c_void_p, c_size_t, c_void_p]),
+    "reflex_sizeof_sample_params": (c_size_t, []),
+    "reflex_sample_workspace_size": (c_size_t, [c_int, c_int]),
+    "reflex_sample_tokens": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p,
+                                     ctypes.POINTER(SampleParamsC), c_int] + [c_void_p] * 3
+                             + [c_size_t, c_void_p]),
 }
 
 N_STAGE_EVENTS = 9
@@ -93,7 +125,9 @@ def lib():
             fn.restype = res
             fn.argtypes = args
         if L.reflex_sizeof_moe_args() != ctypes.sizeof(MoeArgsC) or \
-                L.reflex_sizeof_alloc_params() != ctypes.sizeof(AllocParamsC):
+                L.reflex_sizeof_alloc_params() != ctypes.sizeof(AllocParamsC) or \
+                L.reflex_sizeof_fp8_experts() != ctypes.sizeof(Fp8ExpertsC) or \
+                L.reflex_sizeof_sample_params() != ctypes.sizeof(SampleParamsC):
             raise RuntimeError("libreflex ABI struct layout does not match the binding")
         _lib = L
     return _lib
@@ -263,3 +297,196 @@ def reflex_moe_forward_timed(args: MoeArgsC, ws, events, stream=None):
            "reflex_moe_forward_timed")
 
 
+
+
+# --------------------------------------------------------------------------------------
+# 8-bit products, masked rows, tokens.  These check what the C call cannot see: element
+# types, shapes, density and that all tensors are on one device, whose current stream they
+# use (also where it is not the current device).
+# --------------------------------------------------------------------------------------
+TYPE_BF16, TYPE_F32 = 0, 1
+
+
+def _codes():
+    import torch
+    return (torch.float8_e4m3fn, torch.uint8)
+
+
+def _want(where, name, t, dtypes, shape):
+    """t: a dense tensor of one of `dtypes` and of `shape` (None: any size there)."""
+    if not isinstance(dtypes, tuple):
+        dtypes = (dtypes,)
+    if t.dtype not in dtypes:
+        raise TypeError(f"{where}: {name} has element type {t.dtype}, not {dtypes[0]}")
+    if t.dim() != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{where}: {name} is not contiguous")
+
+
+def _launch(where, tensors, args, stream):
+    """Call entry point `where` with args and the stream, on the tensors' device."""
+    import torch
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+    if device.type != "cuda":
+        raise ValueError(f"{where}: tensors in device memory, not on {device}")
+    fn = getattr(lib(), where)
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, stream_handle(stream)), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, stream_handle(stream)), where)
+
+
+def _pad4(k):
+    return (k + 511) // 512 * 4
+
+
+def fp8_scale_shape(M, K):
+    """Shape of the scale bytes (uint8) of 8-bit rows [M, K]."""
+    return ((K + 511) // 512, M, 4)
+
+
+def fp8_weight_scale_shape(*shape):
+    """Shape of the scale bytes (uint8) of 8-bit weights [N, K] or [E, N, K]."""
+    *lead, N, K = shape
+    return (*lead, (N + 127) // 128, _pad4(K))
+
+
+def reflex_fp8_scale_bytes(M, K) -> int:
+    return lib().reflex_fp8_scale_bytes(M, K)
+
+
+def reflex_fp8_weight_scale_bytes(N, K) -> int:
+    return lib().reflex_fp8_weight_scale_bytes(N, K)
+
+
+def reflex_select_rows_workspace_size(T) -> int:
+    return lib().reflex_select_rows_workspace_size(T)
+
+
+def reflex_select_rows(masked, rows, n_rows, ws=None, stream=None):
+    import torch
+    where = "reflex_select_rows"
+    T = masked.shape[0]
+    _want(where, "masked", masked, (torch.uint8, torch.bool), (T,))
+    _want(where, "rows", rows, torch.int32, (T,))
+    _want(where, "n_rows", n_rows, torch.int32, (1,))
+    _launch(where, (masked, rows, n_rows, ws),
+            (ptr(masked), T, ptr(rows), ptr(n_rows), ptr(ws),
+             0 if ws is None else ws.numel() * ws.element_size()), stream)
+
+
+def reflex_quantize_fp8(x, q, scale, rows=None, n_rows=None, stream=None):
+    import torch
+    where = "reflex_quantize_fp8"
+    M, K = q.shape
+    _want(where, "x", x, torch.bfloat16, (None, K))
+    _want(where, "q", q, _codes(), (M, K))
+    _want(where, "scale", scale, torch.uint8, fp8_scale_shape(M, K))
+    if rows is not None:
+        _want(where, "rows", rows, torch.int32, (None,))
+        if rows.shape[0] < M:
+            raise ValueError(f"{where}: {rows.shape[0]} rows listed for {M} rows of q")
+    if n_rows is not None:
+        _want(where, "n_rows", n_rows, torch.int32, (1,))
+    _launch(where, (x, q, scale, rows, n_rows),
+            (ptr(x), ptr(rows), ptr(n_rows), x.shape[0], M, K, ptr(q), ptr(scale)), stream)
+
+
+def reflex_quantize_fp8_weight(w, q, scale, stream=None):
+    """w, q [N, K] or [E, N, K]."""
+    import torch
+    where = "reflex_quantize_fp8_weight"
+    shape = tuple(w.shape)
+    if len(shape) not in (2, 3):
+        raise ValueError(f"{where}: w has shape {shape}")
+    _want(where, "w", w, torch.bfloat16, shape)
+    _want(where, "q", q, _codes(), shape)
+    _want(where, "scale", scale, torch.uint8, fp8_weight_scale_shape(*shape))
+    E, N, K = (1,) * (3 - len(shape)) + shape
+    _launch(where, (w, q, scale), (ptr(w), E, N, K, ptr(q), ptr(scale)), stream)
+
+
+def reflex_matmul_fp8(x, x_scale, w, w_scale, out, n_rows=None, stream=None):
+    import torch
+    where = "reflex_matmul_fp8"
+    M, K = x.shape
+    N = w.shape[0]
+    _want(where, "x", x, _codes(), (M, K))
+    _want(where, "x_scale", x_scale, torch.uint8, fp8_scale_shape(M, K))
+    _want(where, "w", w, _codes(), (N, K))
+    _want(where, "w_scale", w_scale, torch.uint8, fp8_weight_scale_shape(N, K))
+    _want(where, "out", out, (torch.float32, torch.bfloat16), (M, N))
+    if n_rows is not None:
+        _want(where, "n_rows", n_rows, torch.int32, (1,))
+    _launch(where, (x, x_scale, w, w_scale, out, n_rows),
+            (ptr(x), ptr(x_scale), ptr(w), ptr(w_scale), ptr(n_rows), M, N, K,
+             TYPE_F32 if out.dtype == torch.float32 else TYPE_BF16, ptr(out)), stream)
+
+
+def reflex_swiglu_fp8_workspace_size(pair_capacity, E, f) -> int:
+    return lib().reflex_swiglu_fp8_workspace_size(pair_capacity, E, f)
+
+
+def reflex_grouped_swiglu_fp8(h, h_scale, sorted_token, expert_offsets, w_gate, w_up, w_down,
+                              s_gate, s_up, s_down, y_sorted, ws, stream=None):
+    import torch
+    where = "reflex_grouped_swiglu_fp8"
+    T, d = h.shape
+    E, f, _ = w_gate.shape
+    cap = y_sorted.shape[0]
+    _want(where, "h", h, _codes(), (T, d))
+    _want(where, "h_scale", h_scale, torch.uint8, fp8_scale_shape(T, d))
+    _want(where, "sorted_token", sorted_token, torch.int32, (cap,))
+    _want(where, "expert_offsets", expert_offsets, torch.int32, (E + 1,))
+    for name, w, s, shape in (("gate", w_gate, s_gate, (E, f, d)), ("up", w_up, s_up, (E, f, d)),
+                              ("down", w_down, s_down, (E, d, f))):
+        _want(where, "w_" + name, w, _codes(), shape)
+        _want(where, "s_" + name, s, torch.uint8, fp8_weight_scale_shape(*shape))
+    _want(where, "y_sorted", y_sorted, torch.bfloat16, (cap, d))
+    _launch(where, (h, h_scale, sorted_token, expert_offsets, w_gate, w_up, w_down, s_gate, s_up,
+                    s_down, y_sorted, ws),
+            (ptr(h), ptr(h_scale), ptr(sorted_token), ptr(expert_offsets), ptr(w_gate), ptr(w_up),
+             ptr(w_down), ptr(s_gate), ptr(s_up), ptr(s_down), T, E, d, f, cap, ptr(y_sorted),
+             ptr(ws), ws.numel() * ws.element_size()), stream)
+
+
+def reflex_workspace_fp8_size(T, E, d, f, f_shared, k_max) -> int:
+    return lib().reflex_workspace_fp8_size(T, E, d, f, f_shared, k_max)
+
+
+def reflex_moe_forward_fp8(args: MoeArgsC, experts: Fp8ExpertsC, ws, stream=None):
+    _check(lib().reflex_moe_forward_fp8(ctypes.byref(args), ctypes.byref(experts), ptr(ws),
+                                        ws.numel() * ws.element_size(), stream_handle(stream)),
+           "reflex_moe_forward_fp8")
+
+
+def reflex_sample_workspace_size(M, V) -> int:
+    return lib().reflex_sample_workspace_size(M, V)
+
+
+def reflex_sample_tokens(logits, u, params: SampleParamsC, tokens, conf=None, rows=None,
+                         n_rows=None, ws=None, stream=None):
+    import torch
+    where = "reflex_sample_tokens"
+    M, V = logits.shape
+    T = tokens.shape[0]
+    _want(where, "logits", logits, (torch.float32, torch.bfloat16), (M, V))
+    _want(where, "u", u, torch.float32, (T,))
+    _want(where, "tokens", tokens, torch.int32, (T,))
+    if conf is not None:
+        _want(where, "conf", conf, torch.float32, (T,))
+    if rows is not None:
+        _want(where, "rows", rows, torch.int32, (None,))
+        if rows.shape[0] < M:
+            raise ValueError(f"{where}: {rows.shape[0]} rows listed for {M} rows of logits")
+    if n_rows is not None:
+        _want(where, "n_rows", n_rows, torch.int32, (1,))
+    _launch(where, (logits, u, tokens, conf, rows, n_rows, ws),
+            (ptr(logits), TYPE_F32 if logits.dtype == torch.float32 else TYPE_BF16, ptr(rows),
+             ptr(n_rows), M, V, ptr(u), ctypes.byref(params), T, ptr(tokens), ptr(conf), ptr(ws),
+             0 if ws is None else ws.numel() * ws.element_size()), stream)

@@ -9,7 +9,7 @@
 #include <mutex>
 #include <vector>
 
-#include "common.h"
+#include "fp8.h"
 
 using namespace rfx;
 
@@ -193,6 +193,7 @@ class SideFork {
 struct Layout {
   size_t logits, k, done, pair_offsets, pair_expert, pair_weight, expert_offsets, sorted_token,
       pair_to_sorted, perm, route_hist, swiglu, y, shared_act, shared_y, total;
+  size_t h8, h8_scale;      // the 8-bit forward's input rows
 };
 
 // An always-on expert as wide as the routed ones rides in their two GEMM launches (its rows
@@ -211,9 +212,10 @@ bool shared_joins(int T, int E, int f, int fs, int kcap) {
   return fs == f && static_cast<long long>(T) * std::max(kcap, 1) <= 5LL * E;
 }
 
-bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L) {
+bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L, bool fp8 = false) {
   if (!valid_T(T) || !valid_E(E) || !valid_d(d) || !valid_f(f)) return false;
   if (fs != 0 && !valid_f(fs)) return false;
+  if (fp8 && (f % F8_BLOCK != 0 || fs % F8_BLOCK != 0)) return false;
   if (!valid_kmax(kcap, E)) return false;
   const size_t cap = static_cast<size_t>(T) * kcap;
   if (cap > static_cast<size_t>(INT32_MAX)) return false;
@@ -238,11 +240,17 @@ bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L) {
   L.route_hist = take(route_fused_sorts(T, E) || route_block_sorts(T, E) ? route_hist_bytes(T, E) : 0);
   const bool joins = shared_joins(T, E, f, fs, kcap);
   const size_t rows = cap + (joins ? T : 0);
-  L.swiglu = take(swiglu_ws_bytes(static_cast<int>(rows), f));
+  auto act_bytes = [&](size_t n, int width) {
+    return fp8 ? swiglu8_ws_bytes(static_cast<int>(n), width) : swiglu_ws_bytes(static_cast<int>(n), width);
+  };
+  if (rows > static_cast<size_t>(INT32_MAX)) return false;
+  L.swiglu = take(act_bytes(rows, f));
   L.y = take(sizeof(uint16_t) * rows * d);
-  L.shared_act = fs && !joins ? take(swiglu_ws_bytes(T, fs)) : o;
+  L.shared_act = fs && !joins ? take(act_bytes(T, fs)) : o;
   L.shared_y = joins ? L.y + sizeof(uint16_t) * cap * d
                      : (fs ? take(sizeof(uint16_t) * static_cast<size_t>(T) * d) : o);
+  L.h8 = fp8 ? take(static_cast<size_t>(T) * d) : o;
+  L.h8_scale = fp8 ? take(reflex_fp8_scale_bytes(T, d)) : o;
   L.total = o;
   return true;
 }
@@ -443,20 +451,31 @@ int reflex_combine(const uint16_t* y_sorted, const int32_t* pair_offsets,
 }
 
 static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes, void* stream,
-                            void* const* ev, bool may_fork = true) {
+                            void* const* ev, bool may_fork = true,
+                            const reflex_fp8_experts* x8 = nullptr) {
   if (a == nullptr || ws == nullptr) return REFLEX_ERR_NULL;
   const int T = a->T, E = a->E, d = a->d, f = a->f, fs = a->f_shared;
   if (!valid_T(T) || !valid_E(E) || !valid_d(d) || !valid_f(f) || fs < 0 || (fs && !valid_f(fs)))
     return REFLEX_ERR_SHAPE;
   if (a->norm_topk != 0 && a->norm_topk != 1) return REFLEX_ERR_PARAM;
-  RFX_TRY(check_ptrs({a->h, a->w_router, a->out, ws, a->w_gate, a->w_up, a->w_down}, 16));
+  RFX_TRY(check_ptrs({a->h, a->w_router, a->out, ws}, 16));
+  if (x8 != nullptr) {
+    RFX_TRY(check_ptrs({x8->w_gate, x8->w_up, x8->w_down}, 16));
+    RFX_TRY(check_ptrs({x8->s_gate, x8->s_up, x8->s_down}, 4));
+    if (fs) {
+      RFX_TRY(check_ptrs({x8->ws_gate, x8->ws_up, x8->ws_down}, 16));
+      RFX_TRY(check_ptrs({x8->ss_gate, x8->ss_up, x8->ss_down}, 4));
+    }
+  } else {
+    RFX_TRY(check_ptrs({a->w_gate, a->w_up, a->w_down}, 16));
+  }
   for (const void* p : {static_cast<const void*>(a->residual_a), static_cast<const void*>(a->residual_b)})
     RFX_TRY(check_opt_ptr(p, 16));
   for (const void* p : {static_cast<const void*>(a->router_bias), static_cast<const void*>(a->k_in),
                         static_cast<const void*>(a->k_out), static_cast<const void*>(a->pairs_out),
                         static_cast<const void*>(a->logits_out)})
     RFX_TRY(check_opt_ptr(p, 4));
-  if (fs) RFX_TRY(check_ptrs({a->ws_gate, a->ws_up, a->ws_down}, 16));
+  if (fs && x8 == nullptr) RFX_TRY(check_ptrs({a->ws_gate, a->ws_up, a->ws_down}, 16));
   // pair capacity T * kcap: kcap = uniform_k when set (caller counts are then clamped
   // to it), else params.k_max
   int kcap;
@@ -477,7 +496,7 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
     if (a->B < 0 || a->B > REFLEX_MAX_TOKENS || (T > 0 && a->B < 1)) return REFLEX_ERR_SHAPE;
   }
   Layout L;
-  if (!make_layout(T, E, d, f, fs, kcap, L)) return REFLEX_ERR_SHAPE;
+  if (!make_layout(T, E, d, f, fs, kcap, L, x8 != nullptr)) return REFLEX_ERR_SHAPE;
   if (ws_bytes < L.total) return REFLEX_ERR_WORKSPACE;
   if (T == 0) return REFLEX_OK;
 
@@ -514,9 +533,21 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
   uint16_t* shared_y_buf = fs ? static_cast<uint16_t*>(at(L.shared_y)) : nullptr;
   uint16_t* shared_act = static_cast<uint16_t*>(at(L.shared_act));
   SideFork side(s);      // declared before any early return below: its exit joins
-  if (fs && !joins && ev == nullptr && may_fork && side.fork())
-    RFX_TRY(launch_swiglu_dense(a->h, a->ws_gate, a->ws_up, a->ws_down, T, d, fs, shared_y_buf,
-                                shared_act, side.side()));
+  // the 8-bit experts' input rows, ahead of the fork
+  uint8_t* h8 = static_cast<uint8_t*>(at(L.h8));
+  uint8_t* h8_scale = static_cast<uint8_t*>(at(L.h8_scale));
+  Fp8Weights w8{}, sh8{};
+  if (x8 != nullptr) {
+    w8 = Fp8Weights{x8->w_gate, x8->w_up, x8->w_down, x8->s_gate, x8->s_up, x8->s_down};
+    sh8 = Fp8Weights{x8->ws_gate, x8->ws_up, x8->ws_down, x8->ss_gate, x8->ss_up, x8->ss_down};
+    RFX_TRY(launch_quantize_rows(a->h, nullptr, nullptr, T, T, d, h8, h8_scale, s));
+  }
+  auto shared_expert = [&](hipStream_t on) {
+    if (x8 != nullptr)
+      return launch_swiglu8_dense(h8, h8_scale, sh8, T, d, fs, shared_y_buf, reinterpret_cast<uint8_t*>(shared_act), on);
+    return launch_swiglu_dense(a->h, a->ws_gate, a->ws_up, a->ws_down, T, d, fs, shared_y_buf, shared_act, on);
+  };
+  if (fs && !joins && ev == nullptr && may_fork && side.fork()) RFX_TRY(shared_expert(side.side()));
   const int32_t* k = a->k_in;
   int32_t* kb = a->k_out ? a->k_out : static_cast<int32_t*>(at(L.k));
   // score source of the route kernel: finished scores, or the K slices' partials
@@ -578,11 +609,18 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
                            sorted_token, pair_to_sorted, at(L.perm), s));
   RFX_TRY(mark(4));
   const int sh_rows = joins ? T : 0;
-  RFX_TRY(launch_swiglu_up(a->h, sorted_token, expert_offsets, a->w_gate, a->w_up, T, E, d, f,
-                           cap, AlwaysOn{a->ws_gate, a->ws_up, cap, sh_rows}, act, s));
-  RFX_TRY(mark(5));
-  RFX_TRY(launch_swiglu_down(expert_offsets, a->w_down, T, E, d, f, cap,
-                             AlwaysOn{a->ws_down, nullptr, cap, sh_rows}, act, y, s));
+  if (x8 != nullptr) {
+    uint8_t* act8 = reinterpret_cast<uint8_t*>(act);
+    const AlwaysOn8 on8{sh8, cap, sh_rows};
+    RFX_TRY(launch_swiglu8_up(h8, h8_scale, sorted_token, expert_offsets, w8, T, E, d, f, cap, on8, act8, s));
+    RFX_TRY(launch_swiglu8_down(expert_offsets, w8, T, E, d, f, cap, on8, act8, y, s));
+  } else {
+    RFX_TRY(launch_swiglu_up(a->h, sorted_token, expert_offsets, a->w_gate, a->w_up, T, E, d, f,
+                             cap, AlwaysOn{a->ws_gate, a->ws_up, cap, sh_rows}, act, s));
+    RFX_TRY(mark(5));
+    RFX_TRY(launch_swiglu_down(expert_offsets, a->w_down, T, E, d, f, cap,
+                               AlwaysOn{a->ws_down, nullptr, cap, sh_rows}, act, y, s));
+  }
   RFX_TRY(mark(6));
   const uint16_t* shared_y = nullptr;
   if (joins) {
@@ -591,10 +629,8 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
     RFX_TRY(side.join());
     shared_y = shared_y_buf;
   } else if (fs) {
-    uint16_t* sy = shared_y_buf;
-    RFX_TRY(launch_swiglu_dense(a->h, a->ws_gate, a->ws_up, a->ws_down, T, d, fs, sy,
-                                shared_act, s));
-    shared_y = sy;
+    RFX_TRY(shared_expert(s));
+    shared_y = shared_y_buf;
   }
   RFX_TRY(mark(7));
   RFX_TRY(launch_combine(y, pair_offsets, pair_to_sorted, pair_weight, shared_y, a->residual_a,
@@ -643,6 +679,136 @@ int reflex_moe_forward_timed(const reflex_moe_args* a, void* ws, size_t ws_bytes
   for (int i = 0; i < n_stage_events; ++i)
     if (stage_events[i] == nullptr) return REFLEX_ERR_NULL;
   return moe_forward_impl(a, ws, ws_bytes, stream, stage_events);
+}
+
+// ---- 8-bit products, masked rows, tokens ----------------------------------------------
+size_t reflex_fp8_scale_bytes(int M, int K) {
+  if (!valid_T(M) || !valid_d(K)) return 0;
+  return 4 * static_cast<size_t>(f8_groups(K)) * M;
+}
+
+size_t reflex_fp8_weight_scale_bytes(int N, int K) {
+  if (!valid_T(N) || !valid_d(K)) return 0;
+  return 4 * static_cast<size_t>(f8_groups(K)) * ((N + F8_BLOCK - 1) / F8_BLOCK);
+}
+
+size_t reflex_select_rows_workspace_size(int T) { return valid_T(T) ? select_ws_bytes(T) : 0; }
+
+int reflex_select_rows(const uint8_t* masked, int T, int32_t* rows, int32_t* n_rows, void* ws,
+                       size_t ws_bytes, void* stream) {
+  RFX_TRY(check_ptr(masked, 1));
+  RFX_TRY(check_ptrs({rows, n_rows}, 4));
+  if (!valid_T(T)) return REFLEX_ERR_SHAPE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (select_ws_bytes(T) > 0) {
+    RFX_TRY(check_ptr(ws, 16));
+    if (ws_bytes < select_ws_bytes(T)) return REFLEX_ERR_WORKSPACE;
+  }
+  if (T == 0) return launch_fill_i32(n_rows, 0, 1, s);
+  return launch_select_rows(masked, T, rows, n_rows, ws, s);
+}
+
+int reflex_quantize_fp8(const uint16_t* x, const int32_t* rows, const int32_t* n_rows, int x_rows,
+                        int M, int K, uint8_t* q, uint8_t* scale, void* stream) {
+  RFX_TRY(check_ptrs({x, q}, 16));
+  RFX_TRY(check_ptr(scale, 4));
+  RFX_TRY(check_opt_ptr(rows, 4));
+  RFX_TRY(check_opt_ptr(n_rows, 4));
+  if (!valid_T(x_rows) || !valid_T(M) || !valid_d(K) || (rows == nullptr && x_rows < M))
+    return REFLEX_ERR_SHAPE;
+  if (M == 0) return REFLEX_OK;
+  return launch_quantize_rows(x, rows, n_rows, x_rows, M, K, q, scale, static_cast<hipStream_t>(stream));
+}
+
+int reflex_quantize_fp8_weight(const uint16_t* w, int E, int N, int K, uint8_t* q, uint8_t* scale,
+                               void* stream) {
+  RFX_TRY(check_ptrs({w, q}, 16));
+  RFX_TRY(check_ptr(scale, 4));
+  if (!valid_E(E) || !valid_T(N) || !valid_d(K)) return REFLEX_ERR_SHAPE;
+  const long long blocks = static_cast<long long>(E) * ((N + F8_BLOCK - 1) / F8_BLOCK) * (K / F8_BLOCK);
+  if (blocks > INT32_MAX) return REFLEX_ERR_SHAPE;
+  if (N == 0) return REFLEX_OK;
+  return launch_quantize_weight(w, E, N, K, q, scale, static_cast<hipStream_t>(stream));
+}
+
+int reflex_matmul_fp8(const uint8_t* x, const uint8_t* x_scale, const uint8_t* w,
+                      const uint8_t* w_scale, const int32_t* n_rows, int M, int N, int K,
+                      int out_type, void* out, void* stream) {
+  RFX_TRY(check_ptrs({x, w, out}, 16));
+  RFX_TRY(check_ptrs({x_scale, w_scale}, 4));
+  RFX_TRY(check_opt_ptr(n_rows, 4));
+  if (!valid_T(M) || !valid_T(N) || !valid_d(K)) return REFLEX_ERR_SHAPE;
+  if (out_type != REFLEX_TYPE_BF16 && out_type != REFLEX_TYPE_F32) return REFLEX_ERR_PARAM;
+  if (M == 0 || N == 0) return REFLEX_OK;
+  return launch_matmul8(x, x_scale, w, w_scale, n_rows, M, N, K, out_type, out, static_cast<hipStream_t>(stream));
+}
+
+size_t reflex_swiglu_fp8_workspace_size(int pair_capacity, int E, int f) {
+  if (pair_capacity < 0 || !valid_E(E) || !valid_f(f) || f % F8_BLOCK != 0) return 0;
+  return swiglu8_ws_bytes(pair_capacity, f);
+}
+
+int reflex_grouped_swiglu_fp8(const uint8_t* h, const uint8_t* h_scale, const int32_t* sorted_token,
+                              const int32_t* expert_offsets, const uint8_t* w_gate,
+                              const uint8_t* w_up, const uint8_t* w_down, const uint8_t* s_gate,
+                              const uint8_t* s_up, const uint8_t* s_down, int T, int E, int d,
+                              int f, int32_t pair_capacity, uint16_t* y_sorted, void* ws,
+                              size_t ws_bytes, void* stream) {
+  RFX_TRY(check_ptrs({h, w_gate, w_up, w_down, y_sorted, ws}, 16));
+  RFX_TRY(check_ptrs({h_scale, s_gate, s_up, s_down, sorted_token, expert_offsets}, 4));
+  if (!valid_T(T) || !valid_E(E) || !valid_d(d) || !valid_f(f) || f % F8_BLOCK != 0 || pair_capacity < 0)
+    return REFLEX_ERR_SHAPE;
+  if (ws_bytes < swiglu8_ws_bytes(pair_capacity, f)) return REFLEX_ERR_WORKSPACE;
+  if (T == 0 || pair_capacity == 0) return REFLEX_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  uint8_t* act = static_cast<uint8_t*>(ws);
+  const Fp8Weights w{w_gate, w_up, w_down, s_gate, s_up, s_down};
+  const AlwaysOn8 none{};
+  RFX_TRY(launch_swiglu8_up(h, h_scale, sorted_token, expert_offsets, w, T, E, d, f, pair_capacity, none, act, s));
+  return launch_swiglu8_down(expert_offsets, w, T, E, d, f, pair_capacity, none, act, y_sorted, s);
+}
+
+size_t reflex_sizeof_fp8_experts(void) { return sizeof(reflex_fp8_experts); }
+
+size_t reflex_workspace_fp8_size(int T, int E, int d, int f, int f_shared, int k_max) {
+  Layout L;
+  return make_layout(T, E, d, f, f_shared, k_max, L, true) ? L.total : 0;
+}
+
+int reflex_moe_forward_fp8(const reflex_moe_args* args, const reflex_fp8_experts* experts, void* ws,
+                           size_t ws_bytes, void* stream) {
+  if (experts == nullptr) return REFLEX_ERR_NULL;
+  return moe_forward_impl(args, ws, ws_bytes, stream, nullptr, true, experts);
+}
+
+size_t reflex_sizeof_sample_params(void) { return sizeof(reflex_sample_params); }
+
+static bool valid_vocab(int V) { return V >= 1 && V <= REFLEX_MAX_VOCAB; }
+
+size_t reflex_sample_workspace_size(int M, int V) { return valid_T(M) && valid_vocab(V) ? sample_ws_bytes(M, V) : 0; }
+
+int reflex_sample_tokens(const void* logits, int logits_type, const int32_t* rows,
+                         const int32_t* n_rows, int M, int V, const float* u,
+                         const reflex_sample_params* params, int T, int32_t* tokens, float* conf,
+                         void* ws, size_t ws_bytes, void* stream) {
+  if (params == nullptr) return REFLEX_ERR_NULL;
+  if (logits_type != REFLEX_TYPE_BF16 && logits_type != REFLEX_TYPE_F32) return REFLEX_ERR_PARAM;
+  RFX_TRY(check_ptr(logits, logits_type == REFLEX_TYPE_F32 ? 4 : 2));
+  RFX_TRY(check_ptrs({u, tokens}, 4));
+  for (const void* p : {static_cast<const void*>(rows), static_cast<const void*>(n_rows), static_cast<const void*>(conf)})
+    RFX_TRY(check_opt_ptr(p, 4));
+  if (!valid_T(M) || !valid_T(T) || !valid_vocab(V)) return REFLEX_ERR_SHAPE;
+  const reflex_sample_params& p = *params;
+  if (!std::isfinite(p.temperature) || p.temperature < 0.0f || p.top_k < 0 || !(p.top_p > 0.0f && p.top_p <= 1.0f) ||
+      !(p.min_p >= 0.0f && p.min_p <= 1.0f))
+    return REFLEX_ERR_PARAM;
+  if (sample_ws_bytes(M, V) > 0) {
+    RFX_TRY(check_ptr(ws, 16));
+    if (ws_bytes < sample_ws_bytes(M, V)) return REFLEX_ERR_WORKSPACE;
+  }
+  if (M == 0 || T == 0) return REFLEX_OK;
+  return launch_sample(logits, logits_type, rows, n_rows, M, V, u, p, T, tokens, conf, ws,
+                       static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

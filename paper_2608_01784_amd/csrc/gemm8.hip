@@ -1,0 +1,752 @@
+// SwiGLU experts and plain products on 8-bit rows and weights (fp8.h), on the f8f6f4 MFMA.
+//
+//  UP:    act[j, :] = quantize(SiLU(x_j W_gate[e]^T) * (x_j W_up[e]^T)),  x_j = h[sorted_token[j]]
+//  DOWN:  y[j, :]   = act[j, :] W_down[e]^T
+//  PLAIN: out[i, :] = x[i, :] W^T, any N, the first n_rows rows
+// Both operands are K-contiguous codes.  Rows of one expert are contiguous; each workgroup counts
+// the experts' M tiles itself from expert_offsets, so no launch shape depends on device-resident
+// counts.  One more expert may follow the routed ones, the always-on one: every token is one of
+// its rows, in token order.  In UP the first half of a tile's weight rows are gate rows and the
+// second half the matching up rows, so gate and up of a column meet in one lane and register.
+//
+// Scales: a K slice of the loop is one block of 128 codes, so it has one scale byte per input
+// row and one per 128 weight rows, and v_mfma_scale_f32_32x32x64_f8f6f4 takes both bytes as they
+// are, at the rate of the unscaled instruction and with no vector instruction between the
+// products.  A lane multiplies the same input rows in every slice: it loads their bytes four
+// slices at once, a group ahead.  The weights' bytes of a whole tile lie in one register, a dword
+// a lane.
+//
+// Precision: the f8f6f4 MFMA adds its 64 products with about 17 bits below the largest of them
+// (measured: 1.4e-5 relative in the 2-norm, whatever K is), far inside the rounding to bf16 or e4m3
+// that follows, but not what an fp32 result promises.  PLAIN with fp32 results therefore widens the
+// codes to bf16 (one instruction for two, scale included; e4m3 numbers times powers of two are bf16
+// numbers) and multiplies on v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are
+// fp32: a quarter of the rate, unnoticed where the weights' stream bounds the product.
+//
+// Data movement: operands go from global memory straight into LDS (16 bytes a lane) through rings
+// of slices.  LDS rows are 128 bytes (8 chunks of 16) with chunk c of row r in slot
+// c ^ ((r / 2) % 8): of the 16 rows that a 16-byte read serves at a time, all (row parity, slot)
+// pairs are distinct, so fragment reads are free of bank conflicts, while a wave's copy writes
+// 1 KB (8 whole rows) contiguously.  Each lane reads chunks fsel and 2 + fsel of its row for the
+// first MFMA of a slice and 4 + fsel and 6 + fsel for the second, of both operands alike (which
+// products of a block meet in one instruction is free).
+//
+// Scheduling: a persistent grid walks a flattened sequence of (tile, slice) steps, so copying
+// ahead continues across tile boundaries.  Tiles are dealt to the 8 XCDs in contiguous runs
+// (workgroup b runs on XCD b % 8).  Of an expert the N tiles of one M tile are adjacent (its
+// gathered rows stay in L2); of a plain product the M tiles of one N tile (the weights are the
+// large operand).
+#include <algorithm>
+#include <type_traits>
+
+#include "fp8.h"
+
+namespace rfx {
+
+namespace {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int G8_XCDS = 8;
+constexpr int G8_BK = F8_BLOCK;                  // bytes of a slice's row
+constexpr int G8_CHUNKS = G8_BK / 16;
+constexpr int G8_OP_ROWS = 64 / G8_CHUNKS;       // rows of one wave's copy (1 KB)
+constexpr int G8_NJ = 2;                         // 32-row weight blocks per wave
+enum Mode { UP, DOWN, PLAIN };
+
+// s_waitcnt vmcnt(N) with expcnt and lgkmcnt left at their maxima (vmcnt in bits [3:0] and
+// [15:14], expcnt [6:4], lgkmcnt [11:8]).
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
+}
+
+// Workgroup barrier without the fences of __syncthreads(), which would drain the copies in
+// flight.  lgkmcnt(0): this wave's LDS reads are done before any wave refills what they read.
+__device__ __forceinline__ void lds_barrier8() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Cache policy of the copies: work-group scope; a line is read once per workgroup.
+constexpr int kCopyPolicy = 1;
+
+// One wave's 1 KB copy with 64-bit addresses.  (Out of line of the kernel's lambdas, so that the
+// host-side pass of the kernel stays valid.)
+__device__ __forceinline__ void copy_far(const uint8_t* src, uint8_t* dst) {
+  __builtin_amdgcn_global_load_lds(src, dst, 16, 0, kCopyPolicy);
+}
+
+// Eight codes times a power of two as bf16 numbers.
+__device__ __forceinline__ bf16x8_t widen8(int lo, int hi, float scale) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ float silu_mul(float g, float u) {
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)) * u;
+}
+
+// Staging of a wave's 32 x 32 output block: row pitch 80 bytes.
+constexpr int G8_STAGE_LD = 80, G8_STAGE = 32 * G8_STAGE_LD;
+
+// Epilogue of one 32 x 32 block: rows row_base .., columns col_base .. of `out`, one bf16
+// rounding.  Lane l, register r holds row l % 32 and column 8 (r/4) + 4 (l/32) + r%4; the block
+// goes through the wave's staging buffer and comes back with 4 lanes per row, so a store writes 16
+// rows of 64 contiguous bytes.  N is a multiple of 8 here.  (Inline assembly: the compiler cannot
+// tell the buffer from the ring that copies in flight write, and would wait for those.)
+__device__ __forceinline__ void store_bf16(const f32x16_t& v, int row_base, int col_base, int row_end, int N,
+                                           uint16_t* __restrict__ out, uint32_t stage) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t wr = stage + (lane & 31) * G8_STAGE_LD + 8 * (lane >> 5);
+  const uint32_t rd = stage + (lane >> 2) * G8_STAGE_LD + 16 * (lane & 3);
+  u32x2_t p[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) p[g] = u32x2_t{pack_bf16x2(v[4 * g], v[4 * g + 1]), pack_bf16x2(v[4 * g + 2], v[4 * g + 3])};
+  u32x4_t r0, r1;
+  asm volatile(
+      "ds_write_b64 %2, %4\n\t"
+      "ds_write_b64 %2, %5 offset:16\n\t"
+      "ds_write_b64 %2, %6 offset:32\n\t"
+      "ds_write_b64 %2, %7 offset:48\n\t"
+      "ds_read_b128 %0, %3\n\t"
+      "ds_read_b128 %1, %3 offset:1280\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r0), "=&v"(r1)
+      : "v"(wr), "v"(rd), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3])
+      : "memory");
+  const int row = row_base + (lane >> 2), col = col_base + 8 * (lane & 3);
+  if (col < N) {
+    if (row < row_end) *reinterpret_cast<u32x4_t*>(out + static_cast<size_t>(row) * N + col) = r0;
+    if (row + 16 < row_end) *reinterpret_cast<u32x4_t*>(out + static_cast<size_t>(row + 16) * N + col) = r1;
+  }
+}
+
+// The same for any N and fp32 or bf16 rows, element by element.
+template <class OUT>
+__device__ __forceinline__ void store_any(const f32x16_t& v, int row_base, int col_base, int row_end, int N,
+                                          OUT* __restrict__ out) {
+  const int lane = threadIdx.x & 63, row = row_base + (lane & 31);
+  if (row >= row_end) return;
+  OUT* const to = out + static_cast<size_t>(row) * N;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int col = col_base + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
+    if (col < N) {
+      if constexpr (sizeof(OUT) == 4)
+        to[col] = v[r];
+      else
+        to[col] = f32_to_bf16(v[r]);
+    }
+  }
+}
+
+// A tile shape: WM x WN waves, MI 32-row pair blocks by 64 weight rows each (wave (wm, wn) has
+// the pair blocks wm, wm + WM, ..: an expert's last tile then shortens all waves alike); rings of
+// A_SLOTS input-row and B_SLOTS weight slices, copied A_SLOTS - 1 and B_SLOTS - 1 steps ahead.
+template <int MI_, int WM_, int WN_, int A_SLOTS_, int B_SLOTS_>
+struct Shape8 {
+  static constexpr int MI = MI_, WM = WM_, WN = WN_, WAVES = WM_ * WN_, A_SLOTS = A_SLOTS_, B_SLOTS = B_SLOTS_;
+  static constexpr int THREADS = 64 * WAVES;
+  static constexpr int BM = 32 * MI * WM, BROWS = 64 * WN;              // pair and weight rows of a tile
+  static constexpr int A_BYTES = BM * G8_BK, B_BYTES = BROWS * G8_BK;   // one slice
+  static constexpr int A_OPS = BM / G8_OP_ROWS / WAVES, B_OPS = BROWS / G8_OP_ROWS / WAVES;   // a wave's copies
+  static constexpr int B_WROWS = BROWS / WAVES;                         // weight rows a wave copies
+  static constexpr size_t LDS = size_t(A_SLOTS) * A_BYTES + size_t(B_SLOTS) * B_BYTES;
+  // Copies that may be in flight when a step starts: those issued after its own input rows
+  // (A_SLOTS - 1 steps ago) and weights (no later than the rows).
+  static constexpr int IN_FLIGHT = (B_SLOTS > A_SLOTS ? B_OPS : 0) + (A_SLOTS - 2) * (A_OPS + B_OPS);
+  static_assert(A_SLOTS >= 2 && B_SLOTS >= A_SLOTS, "shape");
+  static_assert(A_OPS * G8_OP_ROWS * WAVES == BM && B_OPS * G8_OP_ROWS * WAVES == BROWS, "whole copies");
+  static_assert(B_WROWS == 32, "a wave's weight rows are all gate or all up rows");
+  static_assert(WAVES * G8_STAGE <= B_BYTES && 16 * BM <= B_BYTES, "the epilogue's scratch fits a weight slot");
+  static_assert(BROWS == 2 * F8_BLOCK, "UP: a tile holds whole activation blocks");
+  static_assert(4 * (REFLEX_MAX_EXPERTS + 1) <= LDS, "start-up scratch in the rings");
+  static_assert(LDS <= 160 * 1024 && IN_FLIGHT < 64, "LDS and vmcnt range");
+};
+
+struct Args8 {
+  const uint8_t* x;                    // [x_rows, K] codes
+  const uint32_t* x_scale;             // [ceil(K / 512)][x_rows], four blocks' bytes each
+  const int32_t *gather, *expert_offsets;
+  const uint8_t *w0, *w1;              // routed weights [E, N, K]: gate and up (UP), or w0 alone
+  const uint32_t *s0, *s1;             // their scales, a dword per four blocks of a row of blocks
+  const uint8_t *sw0, *sw1;            // the always-on expert's (PLAIN: the weights)
+  const uint32_t *ss0, *ss1;
+  int E, K, N, x_rows, out_rows;       // out_rows: rows the routed experts may write
+  int sh_row0, sh_rows;                // the always-on expert's rows of x (UP: of `out` alone)
+  const int32_t* n_rows;               // PLAIN: on the device, NULL: sh_rows
+  void* out;
+  uint8_t* out_scale;                  // UP: the activation's, [ceil(N / 512)][act_rows][4]
+  int act_rows;
+};
+
+// BIG: x of 2^31 bytes or more, addressed with 64-bit pointers (a buffer resource's byte offset
+// has 32 bits, of which the upper half is kept for skipped copies).
+template <Mode MODE, class S, bool BIG, class OUT>
+__global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
+  constexpr int MI = S::MI, A_OPS = S::A_OPS, B_OPS = S::B_OPS;
+  constexpr bool WIDE = MODE == PLAIN && sizeof(OUT) == 4;       // fp32 results
+  constexpr int BN = MODE == UP ? S::BROWS / 2 : S::BROWS;       // output columns of a tile
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem8[];
+  uint8_t* const a_ring = smem8;
+  uint8_t* const b_ring = smem8 + S::A_SLOTS * S::A_BYTES;
+  const int K = a.K, N = a.N, E = a.E;
+  int sh_rows = a.sh_rows;
+  if (MODE == PLAIN && a.n_rows != nullptr) sh_rows = min(max(a.n_rows[0], 0), sh_rows);
+  const int n_tiles = (N + BN - 1) / BN, nk = K / G8_BK, groups = (nk + 3) / 4;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN;
+  // ---- expert row offsets and the prefix of M tiles, in registers: lane l holds experts l,
+  // l + 64, l + 128, l + 192
+  int toff_r[4] = {}, eo_r[4] = {}, eo_E = 0, m_total = 0;
+  if (MODE != PLAIN) {
+    int* s_eo = reinterpret_cast<int*>(smem8);       // (the rings are empty yet)
+    for (int e = tid; e <= E; e += S::THREADS) s_eo[e] = E > 0 ? a.expert_offsets[e] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int e = lane + 64 * q;
+      eo_r[q] = s_eo[e < E ? e : E];
+      const int n = s_eo[e < E ? e + 1 : E] - eo_r[q];
+      const int tiles = n < 0 ? 0 : (n + S::BM - 1) / S::BM;
+      const int incl = wave_inclusive_scan_i32(tiles, lane);
+      toff_r[q] = e < E ? (m_total + incl - tiles) * n_tiles : INT32_MAX;
+      m_total += __builtin_amdgcn_readlane(incl, 63);
+    }
+    eo_E = __builtin_amdgcn_readfirstlane(s_eo[E]);
+    __syncthreads();     // all scratch reads done before the first copies land
+  }
+  auto table_at = [&](const int (&r)[4], int e) {      // entry e (< 256) of a per-lane table
+    const int q = e >> 6;
+    const int v = q == 0 ? r[0] : (q == 1 ? r[1] : (q == 2 ? r[2] : r[3]));
+    return __builtin_amdgcn_readlane(v, e & 63);
+  };
+  struct Tile {
+    int expert, row0, row_end, n0, rot;      // rot: the K group that the tile starts with
+  };
+  // Tiles of one height, in whole 64-row steps: no tile of few rows at an expert's end.
+  auto height_of = [](int rows, int tiles) {
+    return tiles > 1 ? min(((rows + tiles - 1) / tiles + 63) & ~63, S::BM) : S::BM;
+  };
+  const int sh_m = (sh_rows + S::BM - 1) / S::BM;
+  auto decode = [&](bool always_on, int L) {
+    Tile t;
+    if (MODE == PLAIN || always_on) {
+      // (PLAIN: M inner; an always-on expert: N inner, as the routed ones)
+      const int n = MODE == PLAIN ? L / sh_m : L % n_tiles, m = MODE == PLAIN ? L - n * sh_m : L / n_tiles;
+      const int height = height_of(sh_rows, sh_m);
+      t.expert = E;
+      t.n0 = n * BN;
+      t.row0 = a.sh_row0 + min(m * height, sh_rows);
+      t.row_end = min(a.sh_row0 + sh_rows, t.row0 + height);
+      t.rot = n % groups;
+      return t;
+    }
+    int e = -1;      // four ballots count the experts whose first tile lies at or before L
+#pragma unroll
+    for (int q = 0; q < 4; ++q) e += __popcll(__ballot(toff_r[q] <= L));
+    e = e < 0 ? 0 : e;
+    const int local = L - table_at(toff_r, e), m = local / n_tiles, n = local - m * n_tiles;
+    const int er0 = table_at(eo_r, e), er1 = e + 1 < E ? table_at(eo_r, e + 1) : eo_E;
+    const int height = height_of(er1 - er0, (er1 - er0 + S::BM - 1) / S::BM);
+    t.expert = e;
+    t.n0 = n * BN;
+    t.row0 = er0 + m * height;
+    t.row_end = min(min(er1, a.out_rows), t.row0 + height);
+    if (t.row0 < 0 || t.row0 >= t.row_end) t.row_end = t.row0;   // inconsistent offsets: no rows
+    // Tiles that stream weights at the same time start at different groups of their rows
+    t.rot = (MODE == UP ? n % 2 + 5 * e : n) % groups;
+    return t;
+  };
+  // ---- this workgroup's tiles: a contiguous run of the routed (PLAIN: of all) tiles per XCD,
+  // strided over the XCD's workgroups; ahead of it the XCD's share of the always-on expert's
+  const int xcd = blockIdx.x % G8_XCDS, per_xcd = gridDim.x / G8_XCDS, j0 = blockIdx.x / G8_XCDS;
+  const int sh_tiles = MODE == PLAIN ? 0 : sh_m * n_tiles;
+  const int sh_mine = (max(sh_tiles - xcd, 0) + G8_XCDS - 1) / G8_XCDS;
+  const int run_tiles = (MODE == PLAIN ? sh_m : m_total) * n_tiles;
+  const int chunk = (run_tiles + G8_XCDS - 1) / G8_XCDS;
+  const int r_begin = xcd * chunk, r_mine = max(min(run_tiles - r_begin, chunk), 0);
+  if (j0 >= sh_mine + r_mine) return;
+  const int n_my = (sh_mine + r_mine - j0 + per_xcd - 1) / per_xcd;
+  auto tile_at = [&](int i) {
+    const int j = j0 + i * per_xcd;
+    return j < sh_mine ? decode(true, xcd + G8_XCDS * j) : decode(false, r_begin + j - sh_mine);
+  };
+  // ---- copies: op q of a slice fills rows OP_ROWS q ..; lane L writes row r = OP_ROWS q + L / 8 at
+  // slot L % 8, holding chunk (L % 8) ^ ((r / 2) % 8).  Each loader (input rows, weights) has a
+  // current tile and slice and holds the next tile's setup ready: a tile's K loop takes it
+  // across one tile boundary at most (unless short_k, when setups are made at the boundary).
+  const bool short_k = nk < S::B_SLOTS;
+  auto lane_row = [&](int q) { return q * G8_OP_ROWS + lane / G8_CHUNKS; };
+  auto lane_chunk = [&](int q) { return ((lane % G8_CHUNKS) ^ ((lane_row(q) / 2) % G8_CHUNKS)) * 16; };
+  using Off = typename std::conditional<BIG, size_t, uint32_t>::type;
+  int a_tile = -1, a_k = nk, a_rot = 0, a_ops = 0, na_rot = 0, na_ops = 0;
+  bool na_ready = false, na_gather = false;
+  Off a_off[A_OPS];
+  int na_row[A_OPS];
+  auto set_a = [&](const Tile& t) {
+    const int valid = t.row_end - t.row0;
+    // copies wholly past the expert's last row are not issued; rows past it inside a 32-row block
+    // hold whatever the slot held before, enter only their own row of the product, and are not stored
+    const int n = (valid + G8_OP_ROWS - 1) / G8_OP_ROWS - A_OPS * wave;
+    na_ops = __builtin_amdgcn_readfirstlane(min(max(n, 0), A_OPS));
+    na_rot = t.rot;
+    na_gather = MODE == UP && t.expert != E;
+#pragma unroll
+    for (int j = 0; j < A_OPS; ++j) {
+      const int r = lane_row(A_OPS * wave + j);
+      int src = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
+      if (MODE == UP && !na_gather) src -= a.sh_row0;
+      na_row[j] = src;
+    }
+  };
+  auto gather_a = [&]() {
+    if (MODE == UP && na_ready && na_gather) {
+#pragma unroll
+      for (int j = 0; j < A_OPS; ++j) na_row[j] = a.gather[na_row[j]];
+    }
+  };
+  int b_tile = -1, b_k = nk, b_rot = 0, nb_rot = 0, b_len = 0, nb_len = 0;
+  bool nb_ready = false;
+  uint32_t b_lo = 0, b_hi = 0, nb_lo = 0, nb_hi = 0;
+  uint32_t b_off[2];       // copies j and j + 2 are 16 rows apart and share the swizzle
+#pragma unroll
+  for (int j = 0; j < 2; ++j) b_off[j] = static_cast<uint32_t>(lane_row(j) * K + lane_chunk(B_OPS * wave + j));
+  auto set_b = [&](const Tile& t) {
+    nb_rot = t.rot;
+    constexpr int W = S::B_WROWS, HALF = S::WAVES / 2;
+    const bool second = MODE == UP && wave >= HALF;
+    // rows past N are not copied, and their columns not stored
+    const int row = min(t.n0 + W * (second ? wave - HALF : wave), N);
+    nb_len = min(W, N - row) * K;
+    const uint8_t* base = t.expert == E ? (second ? a.sw1 : a.sw0)
+                                        : (second ? a.w1 : a.w0) + static_cast<size_t>(t.expert) * N * K;
+    const uint64_t at = reinterpret_cast<uint64_t>(base + static_cast<size_t>(row) * K);
+    nb_lo = static_cast<uint32_t>(at);
+    nb_hi = static_cast<uint32_t>(at >> 32);
+  };
+  auto ready_a = [&]() {
+    na_ready = a_tile + 1 < n_my;
+    if (!na_ready) return;
+    set_a(tile_at(a_tile + 1));
+    gather_a();
+  };
+  auto ready_b = [&]() {
+    nb_ready = b_tile + 1 < n_my;
+    if (nb_ready) set_b(tile_at(b_tile + 1));
+  };
+  // The byte offset of a loader's next slice; then it advances (past the workgroup's last tile it
+  // stays on its last slice, so the issue never branches and every address stays in bounds).
+  auto a_next = [&]() {
+    if (a_k == nk) {
+      if (na_ready) {
+        na_ready = false;
+        ++a_tile;
+        a_k = 0;
+        a_rot = 4 * na_rot;
+        a_ops = na_ops;
+#pragma unroll
+        for (int j = 0; j < A_OPS; ++j) {
+          const int src = min(max(na_row[j], 0), a.x_rows - 1);
+          a_off[j] = static_cast<Off>(src) * static_cast<Off>(K) + static_cast<Off>(lane_chunk(A_OPS * wave + j));
+        }
+      } else {
+        a_k = nk - 1;
+      }
+    }
+    const int k = a_k + a_rot;
+    ++a_k;
+    return (k >= nk ? k - nk : k) * G8_BK;
+  };
+  auto b_next = [&]() {
+    if (b_k == nk) {
+      if (nb_ready) {
+        nb_ready = false;
+        ++b_tile;
+        b_k = 0;
+        b_rot = 4 * nb_rot;
+        b_lo = nb_lo;
+        b_hi = nb_hi;
+        b_len = nb_len;
+      } else {
+        b_k = nk - 1;
+      }
+    }
+    const int k = b_k + b_rot;
+    ++b_k;
+    return (k >= nk ? k - nk : k) * G8_BK;
+  };
+  // Input rows go through a resource of the operand's size; a skipped copy gets an offset past it,
+  // which the range check turns into no memory access (no branch in the step).
+  const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(a.x), static_cast<short>(0),
+      BIG ? 0 : static_cast<int>(static_cast<uint32_t>(a.x_rows) * static_cast<uint32_t>(K)), 0x00020000);
+  auto copy_a = [&](int j, uint8_t* slot, int k0) {
+    uint8_t* to = slot + (A_OPS * wave + j) * 1024;
+    if constexpr (BIG) {
+      copy_far(a.x + a_off[j] + k0, to);
+    } else {
+      const uint32_t off = j < a_ops ? a_off[j] + static_cast<uint32_t>(k0) : 0x80000000u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (__attribute__((address_space(3))) void*)to, 16, off, 0, 0,
+                                               kCopyPolicy);
+    }
+  };
+  auto copy_b = [&](int j, uint8_t* slot, int k0) {
+    // the resource is rebuilt from wave-uniform values at each use, so that it lives in scalar registers
+    const uint64_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b_lo)));
+    const uint64_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b_hi)));
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(lo | (hi << 32)), static_cast<short>(0), __builtin_amdgcn_readfirstlane(b_len), 0x00020000);
+    const uint32_t off = b_off[j % 2] + static_cast<uint32_t>(k0 + 16 * (j / 2) * K);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void*)(slot + (B_OPS * wave + j) * 1024), 16, off, 0, 0, kCopyPolicy);
+  };
+  // ---- multiply: pair blocks WM i + wm, weight blocks b_row[j] of the tile
+  const int b_row[G8_NJ] = {MODE == UP ? 32 * wn : 64 * wn, MODE == UP ? S::BROWS / 2 + 32 * wn : 64 * wn + 32};
+  const int frow = lane & 31, fsel = lane >> 5, fx = (frow / 2) % G8_CHUNKS;
+  f32x16_t acc[MI][G8_NJ];
+  // ---- scales: source rows of this lane's row of each pair block, of this tile and of the next;
+  // their bytes of the current group; the weights' bytes of all K (UP: gate and up rows)
+  int s_row[MI], ns_row[MI];
+  uint32_t s_cur[MI], w_cur[2] = {0, 0}, w_next[2] = {0, 0};
+  auto set_scales = [&](const Tile& t) {
+    const int valid = t.row_end - t.row0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int r = 32 * (S::WM * i + wm) + frow;
+      int src = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
+      if (MODE == UP) src = t.expert == E ? src - a.sh_row0 : a.gather[src];
+      ns_row[i] = src;
+    }
+    const int block = min(t.n0 + (MODE == UP ? 0 : 64 * wn), N - 1) / F8_BLOCK;
+    const size_t stride = static_cast<size_t>((N + F8_BLOCK - 1) / F8_BLOCK) * groups;
+#pragma unroll
+    for (int j = 0; j < (MODE == UP ? 2 : 1); ++j) {
+      const uint32_t* base = t.expert == E ? (j ? a.ss1 : a.ss0) : (j ? a.s1 : a.s0) + t.expert * stride;
+      w_next[j] = lane < groups ? base[static_cast<size_t>(block) * groups + lane] : 0u;
+    }
+  };
+  auto load_scale = [&](int i, int row, int group) {
+    row = min(max(row, 0), a.x_rows - 1);
+    s_cur[i] = a.x_scale[static_cast<size_t>(group) * a.x_rows + row];
+  };
+  auto take_scales = [&]() {      // the next tile's become the current tile's
+#pragma unroll
+    for (int i = 0; i < MI; ++i) s_row[i] = ns_row[i];
+    w_cur[0] = w_next[0];
+    w_cur[1] = w_next[1];
+  };
+  // ---- prologue: the copies that the steps before the first would have issued
+  ready_a();
+  for (int q = 0; q < S::B_SLOTS - 1; ++q) {
+    if (b_k == nk) ready_b();
+    const int k = b_next();
+#pragma unroll
+    for (int j = 0; j < B_OPS; ++j) copy_b(j, b_ring + q * S::B_BYTES, k);
+  }
+  for (int q = 0; q < S::A_SLOTS - 1; ++q) {
+    if (q > 0 && a_k == nk) ready_a();
+    const int k = a_next();
+#pragma unroll
+    for (int j = 0; j < A_OPS; ++j) copy_a(j, a_ring + q * S::A_BYTES, k);
+  }
+  Tile t = tile_at(0), next_t = t;
+  set_scales(t);
+  take_scales();
+#pragma unroll
+  for (int i = 0; i < MI; ++i) load_scale(i, s_row[i], t.rot);
+  wait_copies<0>();       // (not in the order that the steps count on)
+  int s = 0;              // steps so far (the rings' slot counter)
+  // The K loop of one tile with NB active pair blocks (0: this wave only copies), group by group;
+  // at its end s_cur holds the next tile's first group.
+  auto k_loop = [&](auto nb_c) {
+    constexpr int NB = decltype(nb_c)::value;
+    auto step = [&](const uint32_t (&sx)[MI], const uint32_t (&sw)[2]) {
+      const int ka = a_next(), kb = b_next();
+      // slice s has landed (copies land in order; other outstanding accesses only lengthen the
+      // wait) and is visible to all waves; the slots that the previous step read are free
+      wait_copies<S::IN_FLIGHT>();
+      lds_barrier8();
+      uint8_t* const An = a_ring + ((s + S::A_SLOTS - 1) % S::A_SLOTS) * S::A_BYTES;
+      uint8_t* const Bn = b_ring + ((s + S::B_SLOTS - 1) % S::B_SLOTS) * S::B_BYTES;
+      const uint8_t* const As = a_ring + (s % S::A_SLOTS) * S::A_BYTES;
+      const uint8_t* const Bs = b_ring + (s % S::B_SLOTS) * S::B_BYTES;
+      auto read = [&](const uint8_t* row, int kk) {
+        const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(row + ((4 * kk + fsel) ^ fx) * 16);
+        const i32x4_t hi = *reinterpret_cast<const i32x4_t*>(row + ((4 * kk + 2 + fsel) ^ fx) * 16);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        i32x8_t af[MI], bf[G8_NJ];
+        if constexpr (NB > 0) {
+#pragma unroll
+          for (int j = 0; j < G8_NJ; ++j) bf[j] = read(Bs + (b_row[j] + frow) * G8_BK, kk);
+#pragma unroll
+          for (int i = 0; i < NB; ++i) af[i] = read(As + (32 * (S::WM * i + wm) + frow) * G8_BK, kk);
+        }
+        if (kk == 0) {
+#pragma unroll
+          for (int j = 0; j < A_OPS; ++j) copy_a(j, An, ka);
+        } else {
+#pragma unroll
+          for (int j = 0; j < B_OPS; ++j) copy_b(j, Bn, kb);
+        }
+        // weights as the MFMA's A operand: a lane ends up with 4 consecutive columns of one row
+        if constexpr (WIDE) {
+          const float sws = __uint_as_float((sw[0] & 0xffu) << 23);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            bf16x8_t wb[G8_NJ];
+#pragma unroll
+            for (int j = 0; j < G8_NJ; ++j) wb[j] = widen8(bf[j][2 * q], bf[j][2 * q + 1], sws);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const bf16x8_t xb = widen8(af[i][2 * q], af[i][2 * q + 1], __uint_as_float((sx[i] & 0xffu) << 23));
+#pragma unroll
+              for (int j = 0; j < G8_NJ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], xb, acc[i][j], 0, 0, 0);
+            }
+          }
+        } else
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int j = 0; j < G8_NJ; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                bf[j], af[i], acc[i][j], 0, 0, 0, static_cast<int>(sw[MODE == UP ? j : 0]), 0, static_cast<int>(sx[i]));
+      }
+    };
+    int g = t.rot;
+    for (int done = 0; done < nk;) {
+      const int len = min(4, nk - 4 * g);
+      const bool last = done + len >= nk;
+      uint32_t sx[MI], sw[2];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) sx[i] = s_cur[i];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) sw[j] = __builtin_amdgcn_readlane(static_cast<int>(w_cur[j]), g);
+      if (done == 0 && !short_k) gather_a();
+      g = last ? next_t.rot : (g + 1 < groups ? g + 1 : 0);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) load_scale(i, last ? ns_row[i] : s_row[i], g);
+      for (int q = 0; q < len; ++q, ++s) {
+        step(sx, sw);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sx[i] >>= 8;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) sw[j] >>= 8;
+      }
+      done += len;
+    }
+    take_scales();
+  };
+  for (int tile_i = 0; tile_i < n_my; ++tile_i) {
+    const bool more = tile_i + 1 < n_my;
+    if (more) next_t = tile_at(tile_i + 1);
+    if (short_k) {
+      ready_a();
+      ready_b();
+    } else {
+      na_ready = nb_ready = more;
+      if (more) {
+        set_a(next_t);
+        set_b(next_t);
+      }
+    }
+    set_scales(next_t);
+    // pair blocks of this wave that hold pairs: blocks wm, wm + WM, .. of the tile
+    const int blocks = (t.row_end - t.row0 + 31) >> 5;
+    const int nb = __builtin_amdgcn_readfirstlane(min(max(blocks - wm + S::WM - 1, 0) / S::WM, MI));
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < G8_NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    switch (nb) {      // one instance of the K loop per count of active blocks
+      case 4:
+        if constexpr (MI >= 4) k_loop(std::integral_constant<int, 4>{});
+        break;
+      case 3:
+        if constexpr (MI >= 3) k_loop(std::integral_constant<int, 3>{});
+        break;
+      case 2:
+        if constexpr (MI >= 2) k_loop(std::integral_constant<int, 2>{});
+        break;
+      case 1: k_loop(std::integral_constant<int, 1>{}); break;
+      default: k_loop(std::integral_constant<int, 0>{}); break;
+    }
+    // every wave has read the tile's last slices: the weight slot takes the epilogue's scratch (the
+    // next tile's first step refills it only after its own barrier)
+    lds_barrier8();
+    const uint32_t scratch = static_cast<uint32_t>(
+        reinterpret_cast<uintptr_t>(b_ring + ((s + S::B_SLOTS - 1) % S::B_SLOTS) * S::B_BYTES));
+    if constexpr (MODE == UP) {
+      // the activation and its rows' maxima over this wave's 32 columns; then the codes, with the
+      // maximum of the four waves that share the rows
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        if (i < nb) {
+          uint32_t m = 0, lo, hi;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float v = silu_mul(acc[i][0][r], acc[i][1][r]);
+            acc[i][0][r] = v;
+            const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+            m = max(m, b < 0x7f800000u ? b : 0u);
+          }
+          rows_swap32(m, lo, hi);
+          asm volatile("ds_write_b32 %0, %1" ::"v"(scratch + 16u * (32 * (S::WM * i + wm) + frow) + 4u * wn),
+                       "v"(max(lo, hi)) : "memory");
+        }
+      }
+      lds_barrier8();
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        if (i < nb) {
+          const int in_tile = 32 * (S::WM * i + wm) + frow, row = t.row0 + in_tile;
+          u32x4_t m4;
+          asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(m4) : "v"(scratch + 16u * in_tile) : "memory");
+          const uint32_t byte = f8_scale_byte(max(max(m4[0], m4[1]), max(m4[2], m4[3])));
+          const float inv = f8_inverse(byte);
+          uint32_t v[4];
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const f32x16_t& c = acc[i][0];
+            v[g] = f8_pack4(c[4 * g] * inv, c[4 * g + 1] * inv, c[4 * g + 2] * inv, c[4 * g + 3] * inv);
+#pragma unroll
+            for (int h = 0; h < 4; ++h)       // infinities and NaN: the one NaN code
+              if ((__float_as_uint(c[4 * g + h]) & 0x7fffffffu) >= 0x7f800000u)
+                v[g] = (v[g] & ~(0xffu << (8 * h))) | (0x7fu << (8 * h));
+          }
+          // a lane holds columns 8 g + 4 fsel ..; with the wave's halves swapped the lower one holds
+          // columns 0-15 of each row, the upper one 16-31
+          const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+          const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+          if (row < t.row_end) {
+            uint8_t* to = static_cast<uint8_t*>(a.out) + static_cast<size_t>(row) * N + t.n0 + 32 * wn + 16 * fsel;
+            *reinterpret_cast<u32x4_t*>(to) = u32x4_t{p[0], p[1], q[0], q[1]};
+            const int kb = t.n0 / F8_BLOCK;
+            if (wn == 0 && fsel == 0)
+              a.out_scale[(static_cast<size_t>(kb >> 2) * a.act_rows + row) * 4 + (kb & 3)] = static_cast<uint8_t>(byte);
+          }
+        }
+      }
+    } else {
+      OUT* const out = static_cast<OUT*>(a.out);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        if (i < nb) {
+          const int rb = t.row0 + 32 * (S::WM * i + wm);
+#pragma unroll
+          for (int j = 0; j < G8_NJ; ++j) {
+            const int cb = t.n0 + 64 * wn + 32 * j;
+            if constexpr (MODE == PLAIN)
+              store_any(acc[i][j], rb, cb, t.row_end, N, out);
+            else
+              store_bf16(acc[i][j], rb, cb, t.row_end, N, out, scratch + wave * G8_STAGE);
+          }
+        }
+      }
+    }
+    t = next_t;
+  }
+  wait_copies<0>();     // the last (unused) copies land before the workgroup's LDS is released
+}
+
+// The tile shapes (pair rows x weight rows).  The activation's blocks of 128 columns need 256
+// weight rows a tile (128 of gate, 128 of up).
+using Tall = Shape8<4, 2, 4, 2, 3>;       // 256 x 256, 160 KB of LDS, one workgroup per CU
+using Half = Shape8<2, 2, 4, 3, 3>;       // 128 x 256, 144 KB
+using Quarter = Shape8<1, 2, 4, 3, 4>;    // 64 x 256, 152 KB
+
+template <Mode MODE, class S, bool BIG, class OUT>
+int launch_as(const Args8& a, hipStream_t s) {
+  auto* kernel = &fp8_gemm_kernel<MODE, S, BIG, OUT>;
+  static bool attr_set = false;
+  if (!attr_set) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            static_cast<int>(S::LDS)) != hipSuccess)
+      return REFLEX_ERR_LAUNCH;
+    attr_set = true;
+  }
+  const int grid = (device_cus() + G8_XCDS - 1) / G8_XCDS * G8_XCDS;      // one workgroup per CU
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::THREADS), S::LDS, s, a);
+  return launch_status();
+}
+
+// rows: the most rows an expert is expected to have.
+template <Mode MODE, class OUT>
+int launch_gemm8(const Args8& a, int rows, hipStream_t s) {
+  if (static_cast<size_t>(a.x_rows) * static_cast<size_t>(a.K) >= (size_t(1) << 31))
+    return launch_as<MODE, Tall, true, OUT>(a, s);
+  if (rows <= Quarter::BM) return launch_as<MODE, Quarter, false, OUT>(a, s);
+  if (rows <= Half::BM) return launch_as<MODE, Half, false, OUT>(a, s);
+  return launch_as<MODE, Tall, false, OUT>(a, s);
+}
+
+const uint32_t* dwords(const uint8_t* p) { return reinterpret_cast<const uint32_t*>(p); }
+
+int expected_rows(int T, int E, int cap, int sh_rows) {
+  const int experts = std::min(E, cap);
+  const int routed = experts > 0 ? std::min(T, (cap + experts - 1) / experts) : 0;
+  return std::max(routed, E == 0 ? sh_rows : 0);
+}
+
+}  // namespace
+
+// codes [rows, f], then their scales
+size_t swiglu8_act_bytes(int rows, int f) { return align_up(std::max<size_t>(static_cast<size_t>(rows) * f, 1)); }
+size_t swiglu8_ws_bytes(int rows, int f) {
+  return swiglu8_act_bytes(rows, f) + align_up(std::max<size_t>(4 * static_cast<size_t>(f8_groups(f)) * rows, 1));
+}
+
+int launch_swiglu8_up(const uint8_t* h, const uint8_t* hs, const int32_t* sorted_token, const int32_t* expert_offsets,
+                      const Fp8Weights& w, int T, int E, int d, int f, int cap, const AlwaysOn8& sh, uint8_t* act,
+                      hipStream_t s) {
+  if (cap <= 0 && sh.rows <= 0) return REFLEX_OK;
+  const int rows = cap + sh.rows;
+  const Args8 a{h, dwords(hs), sorted_token, expert_offsets, w.w_gate, w.w_up, dwords(w.s_gate), dwords(w.s_up),
+                sh.w.w_gate, sh.w.w_up, dwords(sh.w.s_gate), dwords(sh.w.s_up), E, d, f, T, cap, sh.row0, sh.rows,
+                nullptr, act, act + swiglu8_act_bytes(rows, f), rows};
+  return launch_gemm8<UP, uint8_t>(a, expected_rows(T, E, cap, sh.rows), s);
+}
+
+int launch_swiglu8_down(const int32_t* expert_offsets, const Fp8Weights& w, int T, int E, int d, int f, int cap,
+                        const AlwaysOn8& sh, const uint8_t* act, uint16_t* y_sorted, hipStream_t s) {
+  if (cap <= 0 && sh.rows <= 0) return REFLEX_OK;
+  const int rows = cap + sh.rows;
+  const Args8 a{act, dwords(act + swiglu8_act_bytes(rows, f)), nullptr, expert_offsets, w.w_down, nullptr,
+                dwords(w.s_down), nullptr, sh.w.w_down, nullptr, dwords(sh.w.s_down), nullptr, E, f, d, rows, cap,
+                sh.row0, sh.rows, nullptr, y_sorted, nullptr, 0};
+  return launch_gemm8<DOWN, uint16_t>(a, expected_rows(T, E, cap, sh.rows), s);
+}
+
+int launch_swiglu8_dense(const uint8_t* x, const uint8_t* xs, const Fp8Weights& w, int M, int d, int f, uint16_t* y,
+                         uint8_t* act, hipStream_t s) {
+  if (M <= 0) return REFLEX_OK;
+  const AlwaysOn8 sh{w, 0, M};
+  const Fp8Weights none{};
+  int rc = launch_swiglu8_up(x, xs, nullptr, nullptr, none, M, 0, d, f, 0, sh, act, s);
+  if (rc == REFLEX_OK) rc = launch_swiglu8_down(nullptr, none, M, 0, d, f, 0, sh, act, y, s);
+  return rc;
+}
+
+int launch_matmul8(const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws, const int32_t* n_rows,
+                   int M, int N, int K, int out_type, void* out, hipStream_t s) {
+  const Args8 a{x, dwords(xs), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, w, nullptr, dwords(ws), nullptr,
+                0, K, N, M, M, 0, M, n_rows, out, nullptr, 0};
+  return out_type == REFLEX_TYPE_F32 ? launch_gemm8<PLAIN, float>(a, M, s) : launch_gemm8<PLAIN, uint16_t>(a, M, s);
+}
+
+}  // namespace rfx

@@ -1,0 +1,99 @@
+// Masked positions as a list (reflex_select_rows): a stable compaction of the indices of
+// nonzero bytes.
+//
+// A thread holds 16 consecutive bytes, a workgroup of 1024 threads a chunk of 16 KB: prefix
+// counts by a wave scan and a scan of the 16 wave sums, the chunk's indices gathered in LDS
+// and written as one contiguous run.  One chunk is one launch; more are two, the first counting
+// every chunk, the second adding up the counts before its own (at most 1024 of them) itself.
+// Bound by launch latency up to millions of positions (one read of T bytes, one write of 4 n).
+#include "fp8.h"
+
+namespace rfx {
+namespace {
+
+constexpr int SR_THREADS = 1024, SR_WAVES = SR_THREADS / kWave, SR_PER = 16;
+constexpr int SR_CHUNK = SR_THREADS * SR_PER;
+static_assert((REFLEX_MAX_TOKENS + SR_CHUNK - 1) / SR_CHUNK <= SR_THREADS, "a count per thread");
+
+// Bit b: byte 16 tid + b of the chunk at `at` is nonzero (bytes past T: zero).  Whole, 16-byte
+// aligned groups in one load.
+__device__ __forceinline__ uint32_t chunk_bits(const uint8_t* masked, int at, int T) {
+  const int i0 = at + SR_PER * static_cast<int>(threadIdx.x);
+  uint32_t bits = 0;
+  if (i0 + SR_PER <= T && (reinterpret_cast<uintptr_t>(masked + i0) & 15) == 0) {
+    const uint4 v = *reinterpret_cast<const uint4*>(masked + i0);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int b = 0; b < SR_PER; ++b) bits |= ((w[b / 4] >> (8 * (b % 4))) & 0xffu) != 0 ? 1u << b : 0u;
+  } else {
+#pragma unroll
+    for (int b = 0; b < SR_PER; ++b)
+      if (i0 + b < T && masked[i0 + b] != 0) bits |= 1u << b;
+  }
+  return bits;
+}
+
+// Sum over the workgroup, in every thread.
+__device__ __forceinline__ int block_sum(int v, int* s_wave) {
+  v = wave_sum_i32(v);
+  if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = v;
+  __syncthreads();
+  int sum = 0;
+#pragma unroll
+  for (int x = 0; x < SR_WAVES; ++x) sum += s_wave[x];
+  __syncthreads();
+  return sum;
+}
+
+__global__ __launch_bounds__(SR_THREADS) void select_count_kernel(const uint8_t* __restrict__ masked, int T,
+                                                                  int32_t* __restrict__ counts) {
+  __shared__ int s_wave[SR_WAVES];
+  const int n = block_sum(__popc(chunk_bits(masked, blockIdx.x * SR_CHUNK, T)), s_wave);
+  if (threadIdx.x == 0) counts[blockIdx.x] = n;
+}
+
+// counts NULL: a single chunk.
+__global__ __launch_bounds__(SR_THREADS) void select_rows_kernel(
+    const uint8_t* __restrict__ masked, int T, const int32_t* __restrict__ counts,
+    int32_t* __restrict__ rows, int32_t* __restrict__ n_rows) {
+  __shared__ int s_wave[SR_WAVES];
+  __shared__ int s_rows[SR_CHUNK];
+  const int tid = threadIdx.x, chunk = blockIdx.x, at = chunk * SR_CHUNK;
+  uint32_t bits = chunk_bits(masked, at, T);
+  const int before = counts == nullptr ? 0 : block_sum(tid < chunk ? counts[tid] : 0, s_wave);
+  const int n = __popc(bits);
+  const int incl = wave_inclusive_scan_i32(n, tid & 63);
+  if ((tid & 63) == 63) s_wave[tid >> 6] = incl;
+  __syncthreads();
+  int pos = incl - n, total = 0;
+#pragma unroll
+  for (int x = 0; x < SR_WAVES; ++x) {
+    const int c = s_wave[x];
+    pos += x < (tid >> 6) ? c : 0;
+    total += c;
+  }
+  while (bits != 0) {
+    s_rows[pos++] = at + SR_PER * tid + __ffs(bits) - 1;
+    bits &= bits - 1;
+  }
+  __syncthreads();
+  for (int j = tid; j < total; j += SR_THREADS) rows[before + j] = s_rows[j];
+  if (tid == 0 && at + SR_CHUNK >= T) n_rows[0] = before + total;
+}
+
+int chunks_of(int T) { return (T + SR_CHUNK - 1) / SR_CHUNK; }
+
+}  // namespace
+
+size_t select_ws_bytes(int T) { return chunks_of(T) <= 1 ? 0 : align_up(sizeof(int32_t) * chunks_of(T)); }
+
+int launch_select_rows(const uint8_t* masked, int T, int32_t* rows, int32_t* n_rows, void* ws, hipStream_t s) {
+  const int chunks = chunks_of(T);
+  int32_t* counts = chunks > 1 ? static_cast<int32_t*>(ws) : nullptr;
+  if (counts != nullptr)
+    hipLaunchKernelGGL(select_count_kernel, dim3(chunks), dim3(SR_THREADS), 0, s, masked, T, counts);
+  hipLaunchKernelGGL(select_rows_kernel, dim3(chunks), dim3(SR_THREADS), 0, s, masked, T, counts, rows, n_rows);
+  return launch_status();
+}
+
+}  // namespace rfx
