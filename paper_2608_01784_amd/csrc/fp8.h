@@ -34,6 +34,36 @@ RFX_DEVICE uint32_t f8_pack4(float a, float b, float c, float d) {
   return static_cast<uint32_t>(v);
 }
 
+// Inclusive prefix sums of 64-bit numbers across a wave, as wave_inclusive_scan_i32 (lanes without a
+// source add zero).
+template <int CTRL, int ROWS, class T>
+RFX_DEVICE T dpp_add64(T v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(u)), CTRL, ROWS, 0xf, false));
+  const uint32_t hi = static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(u >> 32)), CTRL, ROWS, 0xf, false));
+  return v + __builtin_bit_cast(T, (static_cast<uint64_t>(hi) << 32) | lo);
+}
+template <class T>
+RFX_DEVICE T wave_inclusive_scan64(T v) {
+  static_assert(sizeof(T) == 8, "64-bit numbers");
+  v = dpp_add64<0x111, 0xf>(v);      // row_shr:1, 2, 4, 8
+  v = dpp_add64<0x112, 0xf>(v);
+  v = dpp_add64<0x114, 0xf>(v);
+  v = dpp_add64<0x118, 0xf>(v);
+  v = dpp_add64<0x142, 0xa>(v);      // row_bcast:15 to rows 1, 3
+  return dpp_add64<0x143, 0xc>(v);   // row_bcast:31 to rows 2, 3
+}
+// The sum over the wave, in every lane.
+template <class T>
+RFX_DEVICE T wave_sum64(T v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, wave_inclusive_scan64(v));
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(u)), 63));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(u >> 32)), 63));
+  return __builtin_bit_cast(T, (static_cast<uint64_t>(hi) << 32) | lo);
+}
+
 // Scales are kept in groups of four blocks (512 columns).
 __host__ __device__ inline int f8_groups(int K) { return (K + 4 * F8_BLOCK - 1) / (4 * F8_BLOCK); }
 

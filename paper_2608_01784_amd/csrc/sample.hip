@@ -4,42 +4,62 @@
 // token is a matter of which side of a border u lies on, and sums in fp32 (relative error 1e-7
 // times some) would take another token in one row of a hundred where 1e5 tokens share the mass.
 // w = 2^((l - max) log2(e) / temperature) by a table of 64 powers and a cubic (relative error
-// 4e-11, a dozen vector instructions); the confidence's denominator sums fp32 powers.
+// 4e-11, some 15 vector instructions); the confidence's denominator sums fp32 powers.
 //
-// One workgroup of 16 waves holds a row, wave w the w-th sixteenth of it, in 16-byte loads.
-//  1. One pass: maximum with its first index, sum of weights, sum for the confidence.  Every
-//     thread sums relative to a logit of its own, which it moves when one lies 2^60 above it;
-//     the sums are scaled to the row's maximum at the end.
-//  2. Filters, if any.  The last kept logit is found by narrowing a range of 32-bit order keys, 11
-//     bits a pass, by counts (top-k) or weights (top-p; fixed point, 2^-43, so that the sums do
-//     not depend on the order of the atomics).  The range starts at a bound that no kept logit
-//     lies below (at_least()); a pass over the row also lists the range's elements in LDS, in index
-//     order, and when they fit (4096), as they mostly do, everything that follows works on the list.
-//  3. The draw: the kept weights' sums by sixteenth (of the list, or of the row in one more pass),
-//     the one that u falls into, and a scan of that one alone.
+// Launches:
+//  1. The logits are read once from HBM, a wave a part of a row (rows are cut so that few rows fill the
+//     GPU too): each part's maximum with its first index, its sum of weights and its sum for the
+//     confidence.  Every lane sums relative to a logit of its own, which it moves when one lies 2^24
+//     above it.  Groups of eight lanes leave their maxima, from which a bound for top-k follows.
+//  2. With filters: each part's elements above a bound that no kept logit lies below are listed, in
+//     index order, if they are few enough, as they mostly are.
+//  3. A workgroup of 16 waves a row.  Without filters it finds the part that u falls into and scans that
+//     one.  The last kept logit of top-k and top-p is found by counts or weights (fixed point, so that
+//     the sums do not depend on the order of the atomics) in 2048 bins, first linear ones between the
+//     bound and the maximum, then over the 32-bit order keys of one bin, on the list where there is one,
+//     else in passes over the row (in the memory-side cache by then), until what is left fits a list.
+//     The draw goes over the list, or over the row's sixteenths and a scan of one.
 // Everything is inlined and in registers: no stack.
+#include <algorithm>
 #include <cmath>
 #include <limits>
+#include <type_traits>
 
 #include "fp8.h"
 
 namespace rfx {
 namespace {
 
-constexpr int SP_THREADS = 1024, SP_WAVES = SP_THREADS / kWave;
+constexpr int SS_THREADS = 256, SS_WAVES = SS_THREADS / kWave;      // first launch
+constexpr int SP_THREADS = 1024, SP_WAVES = SP_THREADS / kWave;     // second launch
+constexpr int SP_PARTS = 256;                                       // most parts of a row
 constexpr int SP_BIN_BITS = 11, SP_BINS = 1 << SP_BIN_BITS;
 constexpr int SP_LANE = 4, SP_SEG = SP_LANE * kWave;      // list entries of a lane and of a wave
-constexpr double SP_FIXED = 8796093022208.0;              // 2^43: 2^20 weights of 1 fit 64 bits
-static_assert(REFLEX_MAX_VOCAB <= (1 << 20), "fixed-point sums");
-static_assert(SP_BINS == 2 * SP_THREADS, "two bins a thread");
+constexpr int SP_LIST = SP_WAVES * SP_SEG;
+constexpr int SP_SCAN = 8;                                // consecutive elements of a thread in a scan
+static_assert(SP_BINS == 2 * SP_THREADS && SP_PARTS <= SP_THREADS, "two bins a thread");
 constexpr double SP_LOG2E = 1.4426950408889634074;
-constexpr float SP_NONE = -__builtin_huge_valf();
+constexpr float SP_NONE = -__builtin_huge_valf(), SP_LOWEST = -3.402823466e38f;
 
 #define SP_INLINE __attribute__((always_inline))
 
+// What the first launch leaves of a part: sums relative to `top`.
+struct Part {
+  double sum, flat;
+  float top;           // the maximum
+  int first;           // its first index
+  float group[8];      // maxima of the groups of eight lanes
+};
+
+// What the second launch leaves of a part: elements listed, or -1 for too many.
+struct Listed {
+  uint32_t key;
+  int index;
+};
+
 struct SampleArgs {
   const int32_t *rows, *n_rows;
-  int M, V, T;
+  int M, V, T, parts;
   const float* u;
   double scale;          // log2(e) / temperature; 0: temperature 0
   double floor2;         // log2(min_p), -inf for none
@@ -47,626 +67,856 @@ struct SampleArgs {
   double top_p;
   int32_t* tokens;
   float* conf;
+  Part* part;            // [M, parts]
+  int32_t* listed;       // [M, parts]
+  Listed* list;          // [M, SP_LIST]: parts' shares one after the other
 };
 
-// 2^x for -1020 <= x <= 1000.
-RFX_DEVICE double pow2(double x, const double* table) {
-  constexpr double kMagic = 0x1.8p46;            // its last place is 1 / 64
-  const double y = x + kMagic;
-  const double r = x - (y - kMagic);             // |r| <= 1 / 128
-  const int n = static_cast<int>(__double_as_longlong(y));
-  double p = fma(r, 0.05550410866482158, 0.24022650695910071);
-  p = fma(r, p, 0.69314718055994531);
-  p = fma(r, p, 1.0) * table[n & 63];
-  return __longlong_as_double(__double_as_longlong(p) + static_cast<long long>(static_cast<unsigned long long>(n >> 6) << 52));
+constexpr double kMagic = 0x1.8p46;      // its last place is 1 / 64
+
+// a b + c as one instruction with a destination of its own.  (The compiler prefers the form that adds
+// into its destination, and copies the polynomial's constants there for every use.)
+RFX_DEVICE double fma64(double a, double b, double c) {
+#ifdef __HIP_DEVICE_COMPILE__
+  double d;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+#else
+  return fma(a, b, c);
+#endif
+}
+
+// Entry j of the table: 2^(j / 64), its high word less j << 14, so that n << 14 added to it multiplies
+// by 2^((n - j) / 64) for n % 64 = j.
+RFX_DEVICE double pow2_entry(int j) {
+  return __longlong_as_double(__double_as_longlong(exp2(j / 64.0)) - (static_cast<long long>(j) << 46));
+}
+
+// 2^x as a product p t, given y = x + kMagic (rounded) and r = x - (y - kMagic), |r| <= 1 / 128.
+RFX_DEVICE void pow2_parts(double y, double r, const double* table, double& p, double& t) {
+  const uint32_t n = static_cast<uint32_t>(__double_as_longlong(y));      // 64 x, rounded
+  p = fma64(r, fma64(r, fma64(r, 0.05550410866482158, 0.24022650695910071), 0.69314718055994531), 1.0);
+  const uint64_t e = static_cast<uint64_t>(
+      __double_as_longlong(*reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + ((n << 3) & 0x1f8u))));
+  t = __longlong_as_double(static_cast<long long>(((static_cast<uint64_t>(static_cast<uint32_t>(e >> 32) + (n << 14))) << 32) |
+                                                  static_cast<uint32_t>(e)));
+}
+RFX_DEVICE double pow2_of(double y, double r, const double* table) {
+  double p, t;
+  pow2_parts(y, r, table, p, t);
+  return p * t;
 }
 
 // 2^x for x <= 1000, zero below 2^-1020.
-RFX_DEVICE double pow2_or_0(double x, const double* table) { return x >= -1020.0 ? pow2(x, table) : 0.0; }
-
-RFX_DEVICE double wave_sum_f64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
+RFX_DEVICE double pow2_or_0(double x, const double* table) {
+  const double y = x + kMagic;
+  return x >= -1020.0 ? pow2_of(y, x - (y - kMagic), table) : 0.0;
 }
 
+// Of one number a wave in LDS: the sum of those of the waves before wave w, and of all (for every lane).
 template <class T>
-RFX_DEVICE T wave_inclusive_shfl(T v, int lane) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const T up = __shfl_up(v, o, kWave);
-    v += lane >= o ? up : T(0);
+RFX_DEVICE T waves_before(const T* of_wave, int w, T& all) {
+  const int lane = threadIdx.x & 63;
+  const T mine = lane < SP_WAVES ? of_wave[lane] : T(0);
+  all = wave_sum64(mine);
+  return wave_sum64(lane < w ? mine : T(0));
+}
+RFX_DEVICE int waves_before(const int* of_wave, int w, int& all) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < SP_WAVES ? of_wave[lane] : 0;
+  all = wave_sum_i32(mine);
+  return wave_sum_i32(lane < w ? mine : 0);
+}
+
+// A row of logits in parts of whole 16-byte vectors; the elements before the first 16-byte boundary
+// belong to the first part, those behind the last vector to the last.
+template <class E>
+struct Row {
+  static constexpr int VEC = 16 / sizeof(E);
+  typedef float Values __attribute__((ext_vector_type(VEC)));
+  const E* p;
+  int V, head, vecs, parts, per;
+
+  RFX_DEVICE Row(const E* p_, int V_, int parts_) : p(p_), V(V_), parts(parts_) {
+    head = min(V, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(E)));
+    vecs = (V - head) / VEC;
+    per = (vecs + parts - 1) / parts;
   }
-  return v;
+  // First index of a part (parts: V).
+  RFX_DEVICE int begin(int part) const { return part == 0 ? 0 : (part >= parts ? V : head + min(part * per, vecs) * VEC); }
+  RFX_DEVICE float at(int i) const {
+    if constexpr (sizeof(E) == 2)
+      return bf16_to_f32(p[i]);
+    else
+      return p[i];
+  }
+  // A wave's walk over a part, in index order, all 64 lanes in every call: f(values, n, index of the
+  // first, whole), n = VEC, or fewer (0 or 1 too) where `whole` is false_type.  WHOLE: whole waves of
+  // vectors get a call site of their own.
+  template <bool WHOLE, class F>
+  RFX_DEVICE void each(int part, F&& f) const {
+    const int lane = threadIdx.x & 63;
+    const uint4* const vec = reinterpret_cast<const uint4*>(p + head);
+    const int begin = min(part * per, vecs), end = min(begin + per, vecs);
+    auto load = [&](int at) SP_INLINE { return at < end ? vec[at] : make_uint4(0, 0, 0, 0); };
+    auto unpack = [](const uint4& q) SP_INLINE {
+      const uint32_t b[4] = {q.x, q.y, q.z, q.w};
+      Values v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(E) == 2) {
+          v[2 * j] = __uint_as_float(b[j] << 16);
+          v[2 * j + 1] = __uint_as_float(b[j] & 0xffff0000u);
+        } else {
+          v[j] = __uint_as_float(b[j]);
+        }
+      }
+      return v;
+    };
+    int i = begin + lane;
+    uint4 q0 = load(i);      // three vectors ahead
+    uint4 q1 = load(i + kWave);
+    uint4 q2 = load(i + 2 * kWave);
+    uint4 q3 = load(i + 3 * kWave);
+    auto next = [&]() SP_INLINE {
+      q0 = q1;
+      q1 = q2;
+      q2 = q3;
+      q3 = load(i + 4 * kWave);
+      i += kWave;
+    };
+    auto aside = [&](int first, int stop, int& n) SP_INLINE {      // an element a lane
+      Values v;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[j] = SP_NONE;
+      n = first < stop ? 1 : 0;
+      if (n) v[0] = at(first);
+      return v;
+    };
+    const int steps = (end - begin + kWave - 1) / kWave;
+    for (int st = part == 0 ? -1 : 0; st < steps + (part == parts - 1 ? 1 : 0); ++st) {
+      if (WHOLE) {
+        while (st >= 0 && begin + (st + 1) * kWave <= end) {
+          const Values v = unpack(q0);
+          const int first = head + i * VEC;
+          next();
+          f(v, VEC, first, std::true_type{});
+          ++st;
+        }
+        if (st >= steps + (part == parts - 1 ? 1 : 0)) break;
+      }
+      Values v;
+      int n, first;
+      if (st < 0) {
+        first = lane;
+        v = aside(first, head, n);
+      } else if (st == steps) {
+        first = head + vecs * VEC + lane;
+        v = aside(first, V, n);
+      } else {
+        first = head + i * VEC;
+        n = i < end ? VEC : 0;
+        v = unpack(q0);
+        next();
+      }
+      f(v, n, first, std::false_type{});
+    }
+  }
+};
+
+template <class E, bool DRAWS, bool FLAT>      // FLAT: the confidence's sum is another one than the weights'
+__global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __restrict__ logits, SampleArgs a) {
+  constexpr int VEC = Row<E>::VEC;
+  using Values = typename Row<E>::Values;
+  __shared__ double table[64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (DRAWS && tid < 64) table[tid] = pow2_entry(tid);
+  __syncthreads();
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + (tid >> 6));
+  const int j = item / a.parts, part = item - j * a.parts;
+  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
+  const Row<E> row(logits + static_cast<size_t>(j) * a.V, a.V, a.parts);
+  const double scale = a.scale, step = fmax(scale, SP_LOG2E);
+  float best = SP_NONE, ref = SP_LOWEST;
+  int at = 0x7fffffff;
+  double sum = 0.0, flat = 0.0;
+  row.template each<true>(part, [&](Values v, int n, int i, auto whole) SP_INLINE {
+    constexpr bool WHOLE = decltype(whole)::value;
+    // (fmaxf passes NaN by; below, NaN and -inf become the lowest number, whose weight is nothing)
+    float m = fmaxf(v[0], SP_NONE);
+#pragma unroll
+    for (int k = 1; k < VEC; ++k) m = fmaxf(m, v[k]);
+    if ((WHOLE || n > 0) && (m > best || at == 0x7fffffff)) {
+      best = m;
+      at = i;
+#pragma unroll
+      for (int k = VEC - 1; k >= 0; --k)
+        if (v[k] == m) at = i + k;
+      const double up = static_cast<double>(m) - static_cast<double>(ref);
+      if (up * step > 24.0 && m < -SP_NONE) {      // move the reference here
+        if (DRAWS) sum *= pow2_or_0(-up * scale, table);
+        if (FLAT) flat *= exp2(-up * SP_LOG2E);
+        ref = m;
+      }
+    }
+    float z = 0.0f;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const float l = fmaxf(v[k], SP_LOWEST);
+      if (DRAWS) {
+        const double d = static_cast<double>(l) - static_cast<double>(ref);
+        const double y = fmax(fma(d, scale, kMagic), kMagic - 1020.0);
+        double p, t;
+        pow2_parts(y, fma(d, scale, kMagic - y), table, p, t);
+        if (WHOLE)
+          sum = fma(p, t, sum);
+        else
+          sum += k < n ? p * t : 0.0;
+      }
+      if (FLAT) {
+        const float w = __builtin_amdgcn_exp2f((l - ref) * static_cast<float>(SP_LOG2E));
+        z += WHOLE || k < n ? w : 0.0f;
+      }
+    }
+    if (FLAT) flat += static_cast<double>(z);
+  });
+  // maxima of the groups of eight lanes (no elements: -inf)
+  uint32_t group = f32_order_key(best);
+  group = max(group, dpp_u32<kDppXor1>(group));
+  group = max(group, dpp_u32<kDppXor2>(group));
+  group = max(group, dpp_u32<kDppHalfMirror>(group));
+  const uint64_t key =
+      wave_max_u64((static_cast<uint64_t>(f32_order_key(best)) << 32) | (0x7fffffffu - static_cast<uint32_t>(at)));
+  const float top = f32_from_order_key(static_cast<uint32_t>(key >> 32));
+  const double down = fmin(static_cast<double>(ref) - static_cast<double>(top), 0.0);      // (top -inf: +inf)
+  if (DRAWS) sum = wave_sum64(sum * pow2_or_0(down * scale, table));
+  if (FLAT) flat = wave_sum64(flat * exp2(down * SP_LOG2E));
+  if (top == SP_NONE) sum = flat = 0.0;
+  Part* const out = a.part + static_cast<size_t>(j) * a.parts + part;
+  if (lane == 0) {
+    out->sum = sum;
+    out->flat = flat;
+    out->top = top;
+    out->first = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(key));
+  }
+  if (lane % 8 == 0) out->group[lane / 8] = f32_from_order_key(group);
+}
+
+// The bound of a row's filters, by one wave: no kept logit lies below it.
+//  - Top-k: as many groups of lanes as have elements have a maximum each; top_k of them are at least
+//    the bound (its key's low 16 bits zero), so top_k elements are.
+//  - Top-p: the tokens of less than the share (1 - top_p) / V together weigh less than what may be left
+//    out.
+//  - Min-p itself; not where top-p needs the weight of what top-k leaves, min-p's part among it.
+// In fp32, with a margin.  m: the row's maximum, total: its sum of weights.
+RFX_DEVICE float filter_bound(const SampleArgs& a, const Part* part, double m, double total) {
+  const int lane = threadIdx.x & 63, groups = 8 * a.parts;
+  const float top = static_cast<float>(m);
+  const bool by_count = a.top_k < a.V, by_mass = a.top_p < 1.0;
+  float cut = SP_LOWEST;
+  if (by_count && a.top_k <= groups) {
+    uint32_t bound = 0;
+    uint32_t key[8 * SP_PARTS / kWave];
+#pragma unroll
+    for (int q = 0; q < 8 * SP_PARTS / kWave; ++q) {
+      const int g = q * kWave + lane;
+      key[q] = g < groups ? f32_order_key(part[g / 8].group[g % 8]) : 0u;
+    }
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t t = bound | (1u << bit);
+      int n = 0;
+#pragma unroll
+      for (int q = 0; q < 8 * SP_PARTS / kWave; ++q)
+        if (q * kWave < groups) n += __popcll(__ballot(key[q] >= t));
+      if (n >= a.top_k) bound = t;
+    }
+    if (bound > f32_order_key(SP_LOWEST)) cut = f32_from_order_key(bound);
+  } else if (!by_count && by_mass) {
+    cut = static_cast<float>(m + (log2((1.0 - a.top_p) * total / a.V) - 0.001) / a.scale);
+  }
+  if (a.floor2 > -1.0e300 && !(by_count && by_mass)) cut = fmaxf(cut, static_cast<float>(m + (a.floor2 - 0.001) / a.scale));
+  return fminf(fmaxf(cut - 1e-6f * fmaxf(fabsf(cut), fabsf(top)), SP_LOWEST), top);
+}
+
+// A row's maximum and sum of weights from its parts, by one wave.
+RFX_DEVICE void row_sums(const SampleArgs& a, const Part* part, const double* table, float& top, double& total) {
+  const int lane = threadIdx.x & 63;
+  float best = SP_NONE;
+  for (int p = lane; p < a.parts; p += kWave) best = fmaxf(best, part[p].top);
+  top = f32_from_order_key(wave_max_u32(f32_order_key(best)));
+  total = 0.0;
+  for (int p = lane; p < a.parts; p += kWave)
+    total += part[p].sum * pow2_or_0((static_cast<double>(part[p].top) - static_cast<double>(top)) * a.scale, table);
+  total = wave_sum64(total);
+}
+
+template <class E>
+__global__ __launch_bounds__(SS_THREADS) void sample_list_kernel(const E* __restrict__ logits, SampleArgs a) {
+  constexpr int VEC = Row<E>::VEC;
+  using Values = typename Row<E>::Values;
+  __shared__ double table[64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (tid < 64) table[tid] = pow2_entry(tid);
+  __syncthreads();
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + (tid >> 6));
+  const int j = item / a.parts, p = item - j * a.parts;
+  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
+  const Part* const part = a.part + static_cast<size_t>(j) * a.parts;
+  float top;
+  double total;
+  row_sums(a, part, table, top, total);
+  int n_list = -1, room = SP_LIST / a.parts;
+  if (top > SP_NONE && top < -SP_NONE) {
+    const float cut = filter_bound(a, part, top, total);
+    Listed* const list = a.list + static_cast<size_t>(j) * SP_LIST + static_cast<size_t>(p) * room;
+    const Row<E> row(logits + static_cast<size_t>(j) * a.V, a.V, a.parts);
+    n_list = 0;      // (uniform in the wave)
+    row.template each<false>(p, [&](Values v, int n, int i, auto) SP_INLINE {
+      uint32_t on = 0;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) on |= e < n && v[e] >= cut ? 1u << e : 0u;
+      if (__ballot(on != 0) == 0 || n_list > room) return;
+      const int count = __popc(on), incl = wave_inclusive_scan_i32(count, lane);
+      int to = n_list + incl - count;
+      n_list += __builtin_amdgcn_readlane(incl, 63);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        if ((on >> e) & 1u) {
+          if (to < room) list[to] = Listed{f32_order_key(v[e]), i + e};
+          ++to;
+        }
+      }
+    });
+    if (n_list > room) n_list = -1;
+  }
+  if (lane == 0) a.listed[static_cast<size_t>(j) * a.parts + p] = n_list;
 }
 
 struct SampleShared {
   double table[64];
-  double sum[SP_WAVES], flat[SP_WAVES];
+  double sum[SP_WAVES], flat[SP_WAVES], part_sum[SP_PARTS];
   uint64_t best[SP_WAVES], wave_mass[SP_WAVES];
-  int wave_count[SP_WAVES], ties[SP_WAVES], seg_n[SP_WAVES];
-  float low[SP_WAVES];
+  int wave_count[SP_WAVES], ties[SP_WAVES], seg_n[SP_WAVES], part_at[SP_PARTS];
+  uint32_t first[SP_WAVES], last[SP_WAVES];
   double target;
-  uint64_t above_mass;
-  uint32_t bin, above, key_count;
-  int part, token;
-  uint32_t count[SP_BINS];
-  uint64_t mass[SP_BINS];
+  uint64_t above;
+  uint32_t bin;
+  int token;
+  uint64_t hist[SP_BINS];
   uint32_t key[SP_WAVES][SP_SEG];      // the list: order keys and indices, wave w's part in row w
   int index[SP_WAVES][SP_SEG];
 };
 
-// A row of logits: elements before the first 16-byte boundary, vectors, a wave's share of those.
-template <class E>
-struct Row {
-  static constexpr int VEC = 16 / sizeof(E);
-  const E* p;
-  int V, head, vecs, per_wave;
-
-  RFX_DEVICE Row(const E* p_, int V_) : p(p_), V(V_) {
-    head = min(V, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(E)));
-    vecs = (V - head) / VEC;
-    per_wave = (vecs + SP_WAVES - 1) / SP_WAVES;
-  }
-  // First index of wave w's part (w = 16: V).
-  RFX_DEVICE int begin(int w) const { return w == 0 ? 0 : (w == SP_WAVES ? V : head + min(w * per_wave, vecs) * VEC); }
-  // NaN as -inf; inf_row: where some are +inf, those are 0 and the others -inf.
-  RFX_DEVICE static float value(float l, bool inf_row) {
-    l = fmaxf(l, SP_NONE);
-    return inf_row ? (l == -SP_NONE ? 0.0f : SP_NONE) : l;
-  }
-  RFX_DEVICE float at(int i, bool inf_row) const {
-    if constexpr (sizeof(E) == 2)
-      return value(bf16_to_f32(p[i]), inf_row);
-    else
-      return value(p[i], inf_row);
-  }
-  // f(values, n, index of the first) in index order for this wave's part, 64 lanes at a time: n is VEC,
-  // or less (0 and 1 too) before the first and behind the last vector; every lane is active in every call.
-  template <class F>
-  RFX_DEVICE void each(bool inf_row, F&& f) const {
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    float v[VEC];
-    auto single = [&](int i, bool on) SP_INLINE {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) v[j] = SP_NONE;
-      if (on) v[0] = at(i, inf_row);
-      f(v, on ? 1 : 0, i);
-    };
-    if (w == 0) single(lane, lane < head);
-    const uint4* const vec = reinterpret_cast<const uint4*>(p + head);
-    const int begin = min(w * per_wave, vecs), end = min((w + 1) * per_wave, vecs);
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    auto load = [&](int i) SP_INLINE { return i < end ? vec[i] : none; };
-    uint4 q[4];      // three vectors ahead
-#pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = load(begin + j * kWave + lane);
-    for (int i0 = begin; i0 < end; i0 += kWave) {
-      const int i = i0 + lane;
-      const uint32_t b[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
-      q[0] = q[1];
-      q[1] = q[2];
-      q[2] = q[3];
-      q[3] = load(i + 4 * kWave);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (sizeof(E) == 2) {
-          v[2 * j] = value(__uint_as_float(b[j] << 16), inf_row);
-          v[2 * j + 1] = value(__uint_as_float(b[j] & 0xffff0000u), inf_row);
-        } else {
-          v[j] = value(__uint_as_float(b[j]), inf_row);
-        }
-      }
-      f(v, i < end ? VEC : 0, head + i * VEC);
-    }
-    if (w == SP_WAVES - 1) single(head + vecs * VEC + lane, head + vecs * VEC + lane < V);
-  }
-};
-
-template <class E>
+template <class E, bool FILTERS>
 __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict__ logits, SampleArgs a) {
   constexpr int VEC = Row<E>::VEC;
+  using Values = typename Row<E>::Values;
   __shared__ SampleShared s;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int j = blockIdx.x, V = a.V;
+  const int j = blockIdx.x, V = a.V, parts = a.parts;
   const double scale = a.scale, least = a.floor2;
   const int used = a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M);
   if (j >= used) return;
   const int pos = a.rows == nullptr ? j : a.rows[j];
   if (pos < 0 || pos >= a.T) return;
-  if (tid < 64) s.table[tid] = exp2(tid / 64.0);
-  __syncthreads();
-  const Row<E> row(logits + static_cast<size_t>(j) * V, V);
-  const bool draws = scale > 0.0, same = scale == SP_LOG2E;
-  const double step = fmax(scale, SP_LOG2E);
+  if (tid < 64) s.table[tid] = pow2_entry(tid);
+  const Row<E> row(logits + static_cast<size_t>(j) * V, V, SP_WAVES);      // (a wave a sixteenth)
+  const bool draws = scale > 0.0;
 
-  // ---- 1. maximum and sums
-  bool inf_row = false;
-  float top, low;      // the maximum; the least of the threads' own maxima
-  int first;
-  double flat;
-  for (;;) {
-    float best = SP_NONE, ref = -3.402823466e38f;
-    int at = 0x7fffffff;
-    double sum = 0.0, z = 0.0;
-    row.each(inf_row, [&](const float (&v)[VEC], int n, int i) SP_INLINE {
-      float m = v[0];
-#pragma unroll
-      for (int k = 1; k < VEC; ++k) m = fmaxf(m, v[k]);
-      if (n > 0 && (m > best || at == 0x7fffffff)) {
-        best = m;
-        at = i;
-#pragma unroll
-        for (int k = VEC - 1; k >= 0; --k)
-          if (v[k] == m) at = i + k;
-      }
-      const double up = static_cast<double>(m) - static_cast<double>(ref);
-      if (n > 0 && up * step > 60.0 && m < -SP_NONE) {      // move the reference here
-        sum *= pow2_or_0(-up * scale, s.table);
-        z *= pow2_or_0(-up * SP_LOG2E, s.table);
-        ref = m;
-      }
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        if (k < n) {
-          const double x = static_cast<double>(v[k]) - static_cast<double>(ref);
-          if (draws) sum += pow2_or_0(fmin(x * scale, 60.0), s.table);
-          if (!same) z += __builtin_amdgcn_exp2f(static_cast<float>(x * SP_LOG2E));
-        }
-      }
-    });
-    float mine = best;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mine = fminf(mine, __shfl_xor(mine, o, kWave));
-    const uint64_t key = wave_max_u64((static_cast<uint64_t>(f32_order_key(best)) << 32) |
-                                      (0x7fffffffu - static_cast<uint32_t>(at)));
-    if (lane == 0) {
-      s.best[wv] = key;
-      s.low[wv] = mine;
+  // ---- the row's maximum and sums from its parts'
+  const Part* const part_of = a.part + static_cast<size_t>(j) * parts;
+  Part mine{0.0, 0.0, SP_NONE, 0x7fffffff, {}};
+  if (tid < parts) {
+    mine.sum = part_of[tid].sum;
+    mine.flat = part_of[tid].flat;
+    mine.top = part_of[tid].top;
+    mine.first = part_of[tid].first;
+  }
+  const uint64_t key = wave_max_u64((static_cast<uint64_t>(f32_order_key(mine.top)) << 32) |
+                                    (0x7fffffffu - static_cast<uint32_t>(mine.first)));
+  if (lane == 0) s.best[wv] = key;
+  __syncthreads();
+  const uint64_t most = wave_max_u64(lane < SP_WAVES ? s.best[lane] : 0);
+  const uint32_t key_top = static_cast<uint32_t>(most >> 32);
+  const float top = f32_from_order_key(key_top);
+  if (top == SP_NONE) {        // nothing has weight
+    if (tid == 0) {
+      a.tokens[pos] = -1;
+      if (a.conf != nullptr) a.conf[pos] = 0.0f;
     }
-    __syncthreads();
-    uint64_t most = 0;
-    low = -SP_NONE;
-#pragma unroll
-    for (int x = 0; x < SP_WAVES; ++x) {
-      most = max(most, s.best[x]);
-      low = fminf(low, s.low[x]);
-    }
-    top = f32_from_order_key(static_cast<uint32_t>(most >> 32));
-    first = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(most));
-    __syncthreads();
-    if (top == -SP_NONE) {       // some +inf: once more, among them
-      inf_row = true;
-      continue;
-    }
-    if (top == SP_NONE) {        // nothing has weight
-      if (tid == 0) {
-        a.tokens[pos] = -1;
-        if (a.conf != nullptr) a.conf[pos] = 0.0f;
-      }
-      return;
-    }
-    const double down = static_cast<double>(ref) - static_cast<double>(top);
-    sum = wave_sum_f64(sum * pow2_or_0(down * scale, s.table));
-    z = wave_sum_f64(z * pow2_or_0(down * SP_LOG2E, s.table));
-    if (lane == 0) {
-      s.sum[wv] = sum;
-      s.flat[wv] = same ? sum : z;
-    }
-    __syncthreads();
-    flat = 0.0;
-#pragma unroll
-    for (int x = 0; x < SP_WAVES; ++x) flat += s.flat[x];
-    __syncthreads();
-    break;
+    return;
   }
   const double m = top;
-  auto power = [&](float l) SP_INLINE { return (static_cast<double>(l) - m) * scale; };
-  auto key_power = [&](uint32_t k) SP_INLINE { return power(f32_from_order_key(k)); };
-  int token = first;
+  const bool inf_row = top == -SP_NONE;      // the +inf ones have weight 1, the others none
+  // Powers of two of logits by their keys.
+  auto power = [&](uint32_t k) SP_INLINE {
+    if (inf_row) return k == key_top ? 0.0 : -__builtin_huge_val();
+    return (static_cast<double>(f32_from_order_key(k)) - m) * scale;
+  };
+  auto key_of = [&](float l) SP_INLINE { return f32_order_key(fmaxf(l, SP_NONE)); };      // (NaN as -inf)
+  auto weight = [&](uint32_t k) SP_INLINE { return pow2_or_0(power(k), s.table); };
+  double total, flat;
+  if (inf_row) {
+    double n = 0.0;
+    row.template each<false>(wv, [&](Values v, int count, int, auto) SP_INLINE {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) n += e < count && v[e] == -SP_NONE ? 1.0 : 0.0;
+    });
+    total = flat = wave_sum64(n);
+  } else {
+    const double down = static_cast<double>(mine.top) - m;
+    const double sum = mine.sum * pow2_or_0(down * scale, s.table);
+    if (tid < parts) s.part_sum[tid] = sum;
+    total = wave_sum64(sum);
+    flat = scale == SP_LOG2E ? total : wave_sum64(mine.flat * pow2_or_0(down * SP_LOG2E, s.table));
+  }
+  if (lane == 0) {
+    s.sum[wv] = total;
+    s.flat[wv] = flat;
+  }
+  __syncthreads();
+  waves_before(s.sum, 0, total);
+  waves_before(s.flat, 0, flat);
+  __syncthreads();
+
+  // Of the threads' weights in thread order, the thread that `target` (of_all: times the sum) falls
+  // into: s.target is then what is left of it; else the last thread with weight, s.target inf; -1: none
+  // has weight.  `sum`: all weights.  hit: whether it falls into one.
+  auto pick = [&](double w, double target, bool of_all, double& sum, bool& hit) SP_INLINE {
+    const double incl = wave_inclusive_scan64(w);
+    if (lane == 63) s.sum[wv] = incl;
+    __syncthreads();
+    const double before = waves_before(s.sum, wv, sum);
+    if (of_all) target *= sum;
+    const uint64_t hits = __ballot(w > 0.0 && before + incl > target), any = __ballot(w > 0.0);
+    if (lane == 0) {      // (the first thread counted from the end, so that the largest is meant; 0: none)
+      s.first[wv] = hits != 0 ? SP_THREADS - (kWave * wv + __builtin_ctzll(hits)) : 0;
+      s.last[wv] = any != 0 ? kWave * wv + kWave - __builtin_clzll(any) : 0;
+    }
+    __syncthreads();
+    const int first = static_cast<int>(wave_max_u32(lane < SP_WAVES ? s.first[lane] : 0));
+    const int last = static_cast<int>(wave_max_u32(lane < SP_WAVES ? s.last[lane] : 0));
+    hit = first != 0;
+    const int winner = hit ? SP_THREADS - first : last - 1;
+    if (tid == winner) s.target = hit ? target - (before + incl - w) : __builtin_huge_val();
+    __syncthreads();
+    return winner;
+  };
+  int token = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(most));
   if (draws) {
-    // ---- 2. filters: keys above `border` are kept, and the first `border_ties` of those equal to
-    // it; of both only those with power() >= least
-    const bool some = a.top_k < V || a.top_p < 1.0 || least > -1.0e300;
+    float u = a.u[pos];
+    u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+    // ---- filters: keys above `border` are kept, and the first `border_ties` of those equal to it; of
+    // both only those with power() >= least
+    const bool by_count = a.top_k < V, by_mass = a.top_p < 1.0;
+    const bool some = FILTERS || inf_row;
     uint32_t border = f32_order_key(SP_NONE);
     int border_ties = 0;
     bool listed = false;      // the list holds all elements that may be kept
-    if (some) {
-      // A logit that no kept one lies below: by top-k, as many threads as have elements (1024, or V)
-      // have a maximum of at least `low`; by top-p, tokens of less than the share (1 - top_p) / V
-      // together hold less than what may be left out; and min-p itself.  (fp32 after a margin.)
-      float cut = a.top_k <= min(V / VEC, SP_THREADS) ? low : SP_NONE;
-      if (cut == SP_NONE || a.top_k >= V) {
-        cut = SP_NONE;
-        double total = 0.0;
-        if (a.top_p < 1.0 && a.top_k >= V) {
-          for (int x = 0; x < SP_WAVES; ++x) total += s.sum[x];
-          cut = static_cast<float>(m + (log2((1.0 - a.top_p) * total / V) - 0.001) / scale);
-        }
-      }
-      // (not where top-p needs the weight of what top-k leaves, min-p's part among it)
-      if (least > -1.0e300 && (a.top_k >= V || a.top_p >= 1.0))
-        cut = fmaxf(cut, static_cast<float>(m + (least - 0.001) / scale));
-      cut = cut < top ? cut - 1e-6f * fmaxf(fabsf(cut), fabsf(top)) : top;
-      cut = fminf(cut, top);
-      const uint32_t key_low = f32_order_key(fmaxf(cut, -3.402823466e38f)), key_top = f32_order_key(top);
-      // Lists the elements with keys in [lo, hi], in index order, as long as they fit; and counts and
-      // weighs them by bins of (key - lo) >> shift.
-      auto row_pass = [&](uint32_t lo, uint32_t hi, int shift, bool weigh) SP_INLINE {
-        for (int b = tid; b < SP_BINS; b += SP_THREADS) {
-          s.count[b] = 0;
-          s.mass[b] = 0;
-        }
+    double sum_above = 0.0;   // kept weights of this wave's sixteenth above the elements on the list,
+    bool summed = false;      // which are all that may be the border
+    if (!FILTERS && inf_row) border = key_top - 1;
+    if constexpr (FILTERS) {
+      const float cut = inf_row ? top : filter_bound(a, part_of, m, total);
+      const uint32_t key_low = f32_order_key(cut);
+      // Bins of the first pass: linear in the logit, bin 0 at the cut (so that more is higher), or at
+      // weights of 2^-64, where the lower ones are in it too.
+      const float range = fminf(top - cut, static_cast<float>(64.0 / scale));
+      const float inv = range > 1e-30f ? (SP_BINS - 0.5f) / range : 0.0f;
+      auto linear_bin = [&](float l) SP_INLINE {
+        const float t = inf_row ? 0.0f : (top - l) * inv;
+        return SP_BINS - 1 - static_cast<int>(fminf(t, SP_BINS - 1.0f));
+      };
+      // Weights in fixed point, all together between 2^50 and 2^51.  (By a power of two: equal logits at
+      // the maximum have weight 1 and borders that are exact.)
+      const double fixed = __longlong_as_double((2096ll - (__double_as_longlong(total) >> 52)) << 52);
+      auto fixed_weight = [&](uint32_t k) SP_INLINE {
+        return static_cast<uint64_t>(__double_as_longlong(fma(weight(k), fixed, 0x1p52))) - 0x4330000000000000ull;
+      };
+      enum { LINEAR, KEYS, LIST };
+      int stage = by_count || by_mass ? LINEAR : LIST;
+      int within = -1, shift = 0;
+      uint32_t lo = key_low, hi = key_top;
+      bool weigh = !by_count, have = listed;      // have: the list holds them all
+      auto add = [&](uint32_t k, float l) SP_INLINE {
+        const uint32_t bin = stage == LINEAR ? linear_bin(l) : (k - lo) >> shift;
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin]),
+                  static_cast<unsigned long long>(weigh ? fixed_weight(k) : 1u));
+      };
+      // One pass over the elements with keys in [lo, hi] (within: only those of this linear bin; -1:
+      // all): adds them to the bins, linear ones or those of (key - lo) >> shift, by number or by
+      // weight; over the row it also lists them, in index order, as long as they fit, and over the keys
+      // of the last criterion's bin sums the kept weights above.
+      auto pass = [&]() SP_INLINE {
+        for (int b = tid; b < SP_BINS; b += SP_THREADS) s.hist[b] = 0;
         __syncthreads();
-        int n_list = 0;      // (uniform in the wave)
-        row.each(inf_row, [&](const float (&v)[VEC], int n, int i) SP_INLINE {
-          uint32_t in = 0;
-          uint32_t k[VEC];
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            k[e] = f32_order_key(v[e]);
-            in |= e < n && k[e] >= lo && k[e] <= hi ? 1u << e : 0u;
+        const float lo_f = f32_from_order_key(lo), hi_f = f32_from_order_key(hi);
+        if (have) {
+          const int n = s.seg_n[wv];
+          for (int e = lane; e < n; e += kWave) {
+            const uint32_t k = s.key[wv][e];
+            const float l = f32_from_order_key(k);
+            if (k >= lo && k <= hi && (within < 0 || linear_bin(l) == within)) add(k, l);
           }
-          if (__ballot(in != 0) == 0) return;
-          const int mine = __popc(in), incl = wave_inclusive_scan_i32(mine, lane);
-          int to = n_list + incl - mine;
-          n_list += __builtin_amdgcn_readlane(incl, 63);
+          __syncthreads();
+          return;
+        }
+        const bool sum_up = stage == KEYS && !summed && (weigh || !by_mass);
+        int n_list = 0;      // (uniform in the wave)
+        row.template each<false>(wv, [&](Values v, int n, int i, auto) SP_INLINE {
+          uint32_t on = 0, up = 0;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            if ((in >> e) & 1u) {
-              if (to < SP_SEG) {
-                s.key[wv][to] = k[e];
-                s.index[wv][to] = i + e;
-              }
-              ++to;
-              const uint32_t b = (k[e] - lo) >> shift;
-              atomicAdd(&s.count[b], 1u);
-              if (weigh)
-                atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[b]),
-                          static_cast<unsigned long long>(pow2_or_0(power(v[e]), s.table) * SP_FIXED + 0.5));
+            if (e < n && v[e] >= lo_f) {
+              const int bin = within < 0 ? 0 : linear_bin(v[e]) - within;
+              on |= bin == 0 && v[e] <= hi_f ? 1u << e : 0u;
+              up |= bin > 0 || v[e] > hi_f ? 1u << e : 0u;
             }
+          }
+          if (sum_up && __ballot(up != 0) != 0) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              const double x = (static_cast<double>(v[e]) - m) * scale;
+              if (((up >> e) & 1u) && x >= least) sum_above += pow2_or_0(x, s.table);
+            }
+          }
+          if (__ballot(on != 0) == 0) return;
+          if (n_list <= SP_SEG) {
+            const int count = __popc(on), incl = wave_inclusive_scan_i32(count, lane);
+            int to = n_list + incl - count;
+            n_list += __builtin_amdgcn_readlane(incl, 63);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              if ((on >> e) & 1u) {
+                if (to < SP_SEG) {
+                  s.key[wv][to] = f32_order_key(v[e]);
+                  s.index[wv][to] = i + e;
+                }
+                ++to;
+              }
+            }
+          }
+          if (stage != LIST) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+              if ((on >> e) & 1u) add(f32_order_key(v[e]), v[e]);
           }
         });
         if (lane == 0) s.seg_n[wv] = n_list;
         __syncthreads();
-      };
-      auto list_pass = [&](uint32_t lo, uint32_t hi, int shift, bool weigh) SP_INLINE {
-        for (int b = tid; b < SP_BINS; b += SP_THREADS) {
-          s.count[b] = 0;
-          s.mass[b] = 0;
+        have = __ballot(lane < SP_WAVES && s.seg_n[lane] > SP_SEG) == 0;
+        if (sum_up) {
+          summed = have;
+          if (!have) sum_above = 0.0;
         }
-        __syncthreads();
-        const int n = s.seg_n[wv];
-        for (int e = lane; e < n; e += kWave) {
-          const uint32_t k = s.key[wv][e];
-          if (k >= lo && k <= hi) {
-            const uint32_t b = (k - lo) >> shift;
-            atomicAdd(&s.count[b], 1u);
-            if (weigh)
-              atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[b]),
-                        static_cast<unsigned long long>(pow2_or_0(key_power(k), s.table) * SP_FIXED + 0.5));
-          }
-        }
-        __syncthreads();
       };
-      auto list_fits = [&]() SP_INLINE {
-        bool fits = true;
-#pragma unroll
-        for (int x = 0; x < SP_WAVES; ++x) fits = fits && s.seg_n[x] <= SP_SEG;
-        return fits;
-      };
-      // Sums over all bins above bin SP_BINS - 1 - 2 tid (exclusive), then the first bin from the top
-      // that has elements and reaches the aim, or the last with elements: s.bin, and what is above.
-      auto choose = [&](bool weigh, uint32_t above, uint64_t above_mass, double want) SP_INLINE {
-        const int hi = SP_BINS - 1 - 2 * tid;
-        const int n2 = static_cast<int>(s.count[hi] + s.count[hi - 1]);
-        const uint64_t q2 = weigh ? s.mass[hi] + s.mass[hi - 1] : 0;
-        const int incl = wave_inclusive_scan_i32(n2, lane);
-        const uint64_t incl_q = weigh ? wave_inclusive_shfl(q2, lane) : 0;
-        if (lane == 63) {
-          s.wave_count[wv] = incl;
-          s.wave_mass[wv] = incl_q;
-        }
+      // From the top, the first bin with anything in it that brings the sum of the bins (and `above`)
+      // to the aim, or the last with anything; s.above: the sum before it.  The aim is `want`, or
+      // with `share` that share of all but `less`.
+      auto choose = [&](uint64_t above, double want, double share, uint64_t less) SP_INLINE {
+        const int top_bin = SP_BINS - 1 - 2 * tid;
+        const uint64_t h[2] = {s.hist[top_bin], s.hist[top_bin - 1]};
+        const uint64_t incl = wave_inclusive_scan64(h[0] + h[1]);
+        if (lane == 63) s.wave_mass[wv] = incl;
         if (tid == 0) s.bin = 0;
         __syncthreads();
-        uint32_t c = above + incl - n2, all = above;
-        uint64_t q = above_mass + incl_q - q2;
-#pragma unroll
-        for (int x = 0; x < SP_WAVES; ++x) {
-          c += x < wv ? s.wave_count[x] : 0;
-          q += x < wv ? s.wave_mass[x] : 0;
-          all += s.wave_count[x];
-        }
+        uint64_t all;
+        uint64_t q = above + waves_before(s.wave_mass, wv, all) + incl - h[0] - h[1];
+        all += above;
+        if (share > 0.0) want = share * static_cast<double>(all - less);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t n = s.count[hi - e];
-          const uint64_t w = weigh ? s.mass[hi - e] : 0;
-          const bool before = weigh ? (c == 0 || static_cast<double>(q) < want) : static_cast<double>(c) < want;
-          const bool after = weigh ? static_cast<double>(q + w) >= want : static_cast<double>(c + n) >= want;
-          if (n > 0 && before && (after || c + n == all)) {
-            s.bin = hi - e;
-            s.above = c;
-            s.above_mass = q;
-            s.key_count = n;
+          if (h[e] > 0 && (q == 0 || static_cast<double>(q) < want) &&
+              (static_cast<double>(q + h[e]) >= want || q + h[e] == all)) {
+            s.bin = top_bin - e;
+            s.above = q;
           }
-          c += n;
-          q += w;
+          q += h[e];
         }
         __syncthreads();
+        return want;
       };
-      // Narrows [lo, hi] to the border by count (want elements) or weight (a prefix of `want`); room:
-      // elements equal to the first lo that count (the others were cut off before).
-      auto narrow = [&](uint32_t lo, uint32_t hi, bool weigh, double want, int room, uint32_t& key, int& ties,
-                        bool on_list) SP_INLINE {
-        const uint32_t lo0 = lo;
-        uint32_t above = 0;
-        uint64_t above_mass = 0;
-        bool have = on_list;       // the list holds all of [lo, hi]
-        for (;;) {
+      // Top-k, then top-p of what it leaves: a linear pass, then passes over the keys of its bin, each
+      // over the row until what is left fits the list.  What top-k leaves is listed if it fits; top-p
+      // alone works on with the first pass's list if that fits, min-p alone (and rows with +inf without
+      // top-k and top-p) needs nothing but such a list.
+      uint32_t from = key_low;      // elements below are cut off, of those equal to it all but `room`
+      int room = 0x7fffffff;
+      uint64_t above = 0, less = 0;
+      double want = by_count ? static_cast<double>(a.top_k) : a.top_p * (total * fixed);
+      double share = inf_row && !by_count ? a.top_p : 0.0;
+      if (stage == LIST) border = key_low - 1;
+      for (;;) {
+        if (stage == KEYS) {
           const uint32_t span = hi - lo;
-          const int bits = span == 0 ? 0 : 32 - __builtin_clz(span), shift = bits > SP_BIN_BITS ? bits - SP_BIN_BITS : 0;
-          if (have) {
-            list_pass(lo, hi, shift, weigh);
-          } else {
-            row_pass(lo, hi, shift, weigh);
-            have = list_fits();
-            if (lo == key_low && hi == key_top) listed = have;
-          }
-          if (shift == 0 && lo == lo0) {
-            if (tid == 0 && static_cast<uint32_t>(room) < s.count[0]) {
-              s.mass[0] = s.mass[0] / s.count[0] * static_cast<uint32_t>(room);
-              s.count[0] = room;
-            }
+          const int bits = span == 0 ? 0 : 32 - __builtin_clz(span);
+          shift = bits > SP_BIN_BITS ? bits - SP_BIN_BITS : 0;
+        }
+        pass();
+        if (stage == LIST) {
+          listed = have;
+          if (!by_count || !by_mass) break;
+        } else {
+          if (stage == KEYS && shift == 0 && lo == from && room < 0x7fffffff) {
+            const uint64_t most_here = (weigh ? fixed_weight(lo) : 1u) * static_cast<uint64_t>(room);
+            if (tid == 0) s.hist[0] = min(s.hist[0], most_here);
             __syncthreads();
           }
-          choose(weigh, above, above_mass, want);
-          const uint32_t bin = s.bin;
+          want = choose(above, want, share, less);
+          share = 0.0;
+          const uint32_t at = s.bin;
           above = s.above;
-          above_mass = s.above_mass;
-          const uint32_t n = s.key_count;
-          const double each = weigh ? static_cast<double>(s.mass[bin]) / n : 0.0;
+          const uint64_t here = s.hist[at];
           __syncthreads();
-          lo += bin << shift;
-          hi = min(hi, lo + ((1u << shift) - 1u));
-          if (shift == 0) {
-            key = lo;
-            if (weigh) {
-              const double need = (want - static_cast<double>(above_mass)) / each;
-              ties = each > 0.0 && need < n ? max(1, static_cast<int>(ceil(need))) : static_cast<int>(n);
-            } else {
-              ties = min(static_cast<int>(want) - static_cast<int>(above), static_cast<int>(n));
-            }
-            return;
+          if (stage == LINEAR) {
+            listed = listed || have;      // (all from key_low, or from top-k's border, on)
+            within = static_cast<int>(at);
+            stage = KEYS;
+            continue;
           }
+          lo += at << shift;
+          hi = min(hi, lo + ((1u << shift) - 1u));
+          if (shift > 0) continue;
+          border = lo;
+          if (weigh) {
+            // as many of the border's elements as bring the sum to the aim
+            const double each = static_cast<double>(fixed_weight(lo));
+            border_ties = each > 0.0 ? static_cast<int>(fmax(1.0, fmin(ceil((want - static_cast<double>(above)) / each),
+                                                                       rint(static_cast<double>(here) / each))))
+                                     : 1;
+            break;
+          }
+          border_ties = static_cast<int>(fmin(want - static_cast<double>(above), static_cast<double>(here)));
+          less = here - static_cast<uint64_t>(border_ties);      // (their number yet)
+          if (summed) break;
+          if (!listed) {
+            stage = LIST;
+            within = -1;
+            lo = border;
+            hi = key_top;
+            have = false;
+            continue;
+          }
+          if (!by_mass) break;
         }
-      };
-      int room = 0x7fffffff;
-      uint32_t from = key_low;
-      if (a.top_k < V) {
-        narrow(key_low, key_top, false, static_cast<double>(a.top_k), room, border, border_ties, false);
-        from = border;
+        weigh = true;
+        stage = LINEAR;
+        within = -1;
+        from = lo = border;
+        hi = key_top;
         room = border_ties;
-      }
-      if (a.top_p < 1.0) {
-        // the weight of what top-k leaves (without top-k: of all), in fixed point
-        uint64_t q = 0;
-        auto add = [&](uint32_t k) SP_INLINE {
-          if (k > from || (a.top_k >= V && k == from))
-            q += static_cast<uint64_t>(pow2_or_0(key_power(k), s.table) * SP_FIXED + 0.5);
-        };
-        if (a.top_k >= V) from = f32_order_key(-3.402823466e38f);
-        if (listed && a.top_k < V) {
-          for (int e = lane; e < s.seg_n[wv]; e += kWave) add(s.key[wv][e]);
-        } else {
-          row.each(inf_row, [&](const float (&v)[VEC], int n, int) SP_INLINE {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-              if (e < n) add(f32_order_key(v[e]));
-          });
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) q += __shfl_xor(q, o, kWave);
-        if (lane == 0) s.wave_mass[wv] = q;
-        __syncthreads();
-        q = 0;
-#pragma unroll
-        for (int x = 0; x < SP_WAVES; ++x) q += s.wave_mass[x];
-        __syncthreads();
-        double mass = static_cast<double>(q);
-        if (a.top_k < V) mass += static_cast<double>(static_cast<uint64_t>(pow2_or_0(key_power(border), s.table) * SP_FIXED + 0.5)) * border_ties;
-        narrow(a.top_k < V ? border : key_low, key_top, true, a.top_p * mass, room, border, border_ties, listed);
-      }
-      if (a.top_k >= V && !(a.top_p < 1.0)) {       // min-p alone
-        row_pass(key_low, key_top, 31, false);
-        listed = list_fits();
-        border = key_low - 1;
+        have = listed;
+        above = 0;
+        less *= fixed_weight(border);
+        share = a.top_p;
       }
     }
-    // ---- 3. the draw
+    // ---- the draw
     auto kept = [&](uint32_t k, bool tie_kept) SP_INLINE {
-      return (k > border || (k == border && tie_kept)) && k > f32_order_key(SP_NONE) && key_power(k) >= least;
+      return (k > border || (k == border && tie_kept)) && k > f32_order_key(SP_NONE) && power(k) >= least;
     };
-    float u = a.u[pos];
-    u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
-    // The part that u falls into, from the parts' weights in s.sum: s.part (-1: none has weight), and
-    // what is left of u in s.target.
-    auto choose_part = [&]() SP_INLINE {
+    // Ranks of a thread's `n` ties among all threads' in thread order; `all`: how many there are.
+    auto tie_rank = [&](int n, int& all) SP_INLINE {
+      const int incl = wave_inclusive_scan_i32(n, lane);
+      if (lane == 63) s.wave_count[wv] = incl;
       __syncthreads();
-      if (tid == 0) {
-        double all = 0.0, cum = 0.0, before = 0.0;
-        for (int x = 0; x < SP_WAVES; ++x) all += s.sum[x];
-        const double target = u * all;
-        int part = -1;
-        for (int x = 0; x < SP_WAVES; ++x) {
-          if (s.sum[x] <= 0.0) continue;
-          part = x;
-          before = cum;
-          cum += s.sum[x];
-          if (target < cum) break;
-        }
-        s.part = part;
-        s.target = target < cum ? target - before : __builtin_huge_val();
-      }
+      const int rank = waves_before(s.wave_count, wv, all) + incl - n;
       __syncthreads();
+      return rank;
     };
-    if (some && listed) {
-      // wave w has segment w, lane l its entries 4 l ..
+    // The weights of the list's entries, kept ones: wave w has segment w, lane l its entries 4 l ..;
+    // and how many ties among them are kept.
+    double w[SP_LANE];
+    double sum = 0.0;
+    int ties_kept = 0;
+    if (FILTERS && (listed || summed)) {
       const int n = s.seg_n[wv];
       uint32_t k[SP_LANE];
-      int ties = 0;
+      int ties = 0, all;
 #pragma unroll
       for (int e = 0; e < SP_LANE; ++e) {
         const int at = SP_LANE * lane + e;
         k[e] = at < n ? s.key[wv][at] : 0u;
         ties += k[e] == border ? 1 : 0;
       }
-      int rank = wave_inclusive_scan_i32(ties, lane);
-      if (lane == 63) s.ties[wv] = rank;
-      __syncthreads();
-      rank -= ties;
-      for (int x = 0; x < wv; ++x) rank += s.ties[x];
-      double w[SP_LANE], mine = 0.0;
+      int rank = tie_rank(ties, all);
 #pragma unroll
       for (int e = 0; e < SP_LANE; ++e) {
         const bool tie = k[e] == border;
-        w[e] = kept(k[e], tie && rank < border_ties) ? pow2_or_0(key_power(k[e]), s.table) : 0.0;
+        w[e] = kept(k[e], tie && rank < border_ties) ? weight(k[e]) : 0.0;
+        ties_kept += tie && rank < border_ties ? 1 : 0;
         rank += tie ? 1 : 0;
-        mine += w[e];
+        sum += w[e];
       }
-      const double incl = wave_inclusive_shfl(mine, lane);
-      if (lane == 63) s.sum[wv] = incl;
-      if (tid == 0) s.token = -1;
-      choose_part();
-      if (s.part == wv) {
-        // the first entry past the target, else the last kept one
-        const double target = s.target;
-        double cum = incl - mine;
-        int hit = -1, last = -1;
+    }
+    if (FILTERS && listed) {
+      double sum_all;
+      bool hit;
+      const int winner = pick(sum, u, true, sum_all, hit);
+      if (tid == winner) {
+        double cum = 0.0;
+        int to = -1;
+        bool past = false;
 #pragma unroll
         for (int e = 0; e < SP_LANE; ++e) {
           cum += w[e];
-          if (w[e] > 0.0) {
-            last = SP_LANE * lane + e;
-            if (hit < 0 && cum > target) hit = last;
+          if (w[e] > 0.0 && !past) {
+            to = s.index[wv][SP_LANE * lane + e];
+            past = cum > s.target;
           }
         }
-        const uint64_t hits = __ballot(hit >= 0), any = __ballot(last >= 0);
-        const int to = hits != 0 ? __shfl(hit, __builtin_ctzll(hits), kWave)
-                                 : (any != 0 ? __shfl(last, 63 - __builtin_clzll(any), kWave) : -1);
-        if (lane == 0 && to >= 0) s.token = s.index[wv][to];
+        s.token = to;
       }
       __syncthreads();
-      token = s.token >= 0 ? s.token : token;
+      if (winner >= 0) token = s.token;
     } else {
-      if (some) {
-        double sum = 0.0;
+      int part, begin, end, tie_room = 0;
+      double unused;
+      bool hit;
+      if (FILTERS && summed) {
+        sum = wave_sum64(sum + sum_above);
+        ties_kept = wave_sum_i32(ties_kept);
+        if (lane == 0) s.ties[wv] = ties_kept;
+      } else if (some) {
         int ties = 0;
-        row.each(inf_row, [&](const float (&v)[VEC], int n, int) SP_INLINE {
+        row.template each<false>(wv, [&](Values v, int n, int, auto) SP_INLINE {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            const uint32_t k = f32_order_key(v[e]);
-            if (e < n && kept(k, false)) sum += pow2_or_0(power(v[e]), s.table);
+            const uint32_t k = key_of(v[e]);
+            if (e < n && kept(k, false)) sum += weight(k);
             ties += e < n && k == border ? 1 : 0;
           }
         });
-        sum = wave_sum_f64(sum);
+        sum = wave_sum64(sum);
         ties = wave_sum_i32(ties);
-        if (lane == 0) {
-          s.sum[wv] = sum;
-          s.ties[wv] = ties;
+        if (lane == 0) s.ties[wv] = ties;
+        __syncthreads();
+        int all;
+        const int mine_kept = min(ties, max(border_ties - waves_before(s.ties, wv, all), 0));
+        if (kept(border, true)) sum += mine_kept * weight(border);
+        __syncthreads();
+        if (lane == 0) s.ties[wv] = mine_kept;
+      }
+      if (some) {
+        part = pick(lane == 0 ? sum : 0.0, u, true, unused, hit) / kWave;      // (-1 / 64 is 0: weights are there)
+        tie_room = s.ties[part];
+        begin = row.begin(part);
+        end = row.begin(part + 1);
+      } else {
+        const Row<E> first(row.p, V, parts);
+        part = max(pick(tid < parts ? s.part_sum[tid] : 0.0, u, true, unused, hit), 0);
+        begin = first.begin(part);
+        end = first.begin(part + 1);
+      }
+      // that part, eight consecutive elements a thread; the last kept token stands in where the order
+      // of the additions leaves the target at the part's end
+      double target = s.target;
+      int tie_base = 0;
+      __syncthreads();
+      for (int i0 = begin; i0 < end; i0 += SP_SCAN * SP_THREADS) {
+        const int i1 = i0 + SP_SCAN * tid;
+        uint32_t k[SP_SCAN];
+        int ties = 0, all = 0;
+#pragma unroll
+        for (int e = 0; e < SP_SCAN; ++e) {
+          k[e] = i1 + e < end ? key_of(row.at(i1 + e)) : 0u;
+          ties += k[e] == border ? 1 : 0;
+        }
+        int rank = 0;
+        if (some) rank = tie_base + tie_rank(ties, all);
+        double w[SP_SCAN], sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < SP_SCAN; ++e) {
+          const bool tie = k[e] == border;
+          const bool keep = some ? kept(k[e], tie && rank < tie_room) : k[e] > f32_order_key(SP_NONE);
+          w[e] = keep ? weight(k[e]) : 0.0;
+          rank += tie ? 1 : 0;
+          sum += w[e];
+        }
+        double sum_all;
+        const int winner = pick(sum, target, false, sum_all, hit);
+        if (tid == winner) {
+          double cum = 0.0;
+          int to = -1;
+          bool past = false;
+#pragma unroll
+          for (int e = 0; e < SP_SCAN; ++e) {
+            cum += w[e];
+            if (w[e] > 0.0 && !past) {
+              to = i1 + e;
+              past = cum > s.target;
+            }
+          }
+          s.token = to;
         }
         __syncthreads();
-        if (tid == 0) {
-          const double tie = kept(border, true) ? pow2_or_0(key_power(border), s.table) : 0.0;
-          int left = border_ties;
-          for (int x = 0; x < SP_WAVES; ++x) {
-            const int n = min(s.ties[x], left);
-            s.sum[x] += n * tie;
-            s.ties[x] = n;        // the part's kept ties
-            left -= n;
-          }
-        }
-      }
-      choose_part();
-      const int part = s.part;
-      if (part >= 0) {
-        const double target = s.target;
-        const int end = row.begin(part + 1), tie_room = some ? s.ties[part] : 0;
-        double base = 0.0;
-        int tie_base = 0;
-        // 1024 elements at a time; the last kept token stands in where the order of the additions
-        // leaves the target at the part's end
-        for (int i0 = row.begin(part); i0 < end; i0 += SP_THREADS) {
-          const int i = i0 + tid;
-          const uint32_t k = i < end ? f32_order_key(row.at(i, inf_row)) : 0u;
-          const bool tie = some && k == border;
-          const int tie_incl = wave_inclusive_scan_i32(tie ? 1 : 0, lane);
-          if (lane == 63) s.wave_count[wv] = tie_incl;
-          __syncthreads();
-          int rank = tie_base + tie_incl - 1, tie_all = 0;
-#pragma unroll
-          for (int x = 0; x < SP_WAVES; ++x) {
-            rank += x < wv ? s.wave_count[x] : 0;
-            tie_all += s.wave_count[x];
-          }
-          const bool keep = some ? kept(k, tie && rank < tie_room) : k > f32_order_key(SP_NONE);
-          const double w = keep ? pow2_or_0(key_power(k), s.table) : 0.0;
-          const double incl = wave_inclusive_shfl(w, lane);
-          if (lane == 63) s.flat[wv] = incl;
-          __syncthreads();
-          double before = base, all = base;
-#pragma unroll
-          for (int x = 0; x < SP_WAVES; ++x) {
-            before += x < wv ? s.flat[x] : 0.0;
-            all += s.flat[x];
-          }
-          const uint64_t hits = __ballot(w > 0.0 && before + incl > target), any = __ballot(w > 0.0);
-          if (lane == 0) {
-            const int hit = hits != 0 ? i0 + kWave * wv + __builtin_ctzll(hits) : 0x7fffffff;
-            const int last = any != 0 ? i0 + kWave * wv + 63 - __builtin_clzll(any) : -1;
-            s.best[wv] = (static_cast<uint64_t>(static_cast<uint32_t>(hit)) << 32) | static_cast<uint32_t>(last);
-          }
-          __syncthreads();
-          int hit = 0x7fffffff, last = -1;
-#pragma unroll
-          for (int x = 0; x < SP_WAVES; ++x) {
-            hit = min(hit, static_cast<int>(s.best[x] >> 32));
-            last = max(last, static_cast<int>(static_cast<uint32_t>(s.best[x])));
-          }
-          __syncthreads();
-          if (last >= 0) token = last;
-          if (hit != 0x7fffffff) {
-            token = hit;
-            break;
-          }
-          base = all;
-          tie_base += tie_all;
-        }
+        if (winner >= 0) token = s.token;
+        __syncthreads();
+        if (hit) break;
+        target -= sum_all;
+        tie_base += all;
       }
     }
   }
   if (tid == 0) {
     a.tokens[pos] = token;
-    if (a.conf != nullptr)
-      a.conf[pos] = static_cast<float>(pow2_or_0((static_cast<double>(row.at(token, inf_row)) - m) * SP_LOG2E, s.table) / flat);
+    if (a.conf != nullptr) {
+      const uint32_t k = key_of(row.at(token));
+      const double x = k == key_top ? 0.0 : (static_cast<double>(f32_from_order_key(k)) - m) * SP_LOG2E;
+      a.conf[pos] = static_cast<float>(pow2_or_0(x, s.table) / flat);
+    }
   }
+}
+
+// Parts of a row: 8192 elements at most (a scan's reach), more parts for few rows: a wave each, 4096
+// waves fill the GPU, but not fewer than two vectors a lane.
+int parts_of(int M, int V) {
+  const int least = (V + SP_SCAN * SP_THREADS - 1) / (SP_SCAN * SP_THREADS);
+  const int fill = std::min((4096 + M - 1) / std::max(M, 1), V / (2 * kWave * 4));
+  return std::min(std::max({least, fill, 1}), SP_PARTS);
 }
 
 }  // namespace
 
-size_t sample_ws_bytes(int, int) { return 0; }
+static bool filters(const SampleArgs& a) { return a.top_k < a.V || a.top_p < 1.0 || a.floor2 > -1.0e300; }
+
+// The parts' records, then the numbers of elements listed, then the lists.
+static size_t part_bytes(int M, int V) { return align_up(sizeof(Part) * static_cast<size_t>(M) * parts_of(M, V)); }
+static size_t listed_bytes(int M, int V) { return align_up(sizeof(int32_t) * static_cast<size_t>(M) * parts_of(M, V)); }
+size_t sample_ws_bytes(int M, int V) {
+  return part_bytes(M, V) + listed_bytes(M, V) + align_up(sizeof(Listed) * static_cast<size_t>(M) * SP_LIST);
+}
+
+template <class E>
+static int launch_sample_as(const E* logits, const SampleArgs& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((static_cast<size_t>(a.M) * a.parts + SS_WAVES - 1) / SS_WAVES));
+  if (a.scale == SP_LOG2E)
+    hipLaunchKernelGGL((sample_sums_kernel<E, true, false>), grid, dim3(SS_THREADS), 0, s, logits, a);
+  else if (a.scale > 0.0)
+    hipLaunchKernelGGL((sample_sums_kernel<E, true, true>), grid, dim3(SS_THREADS), 0, s, logits, a);
+  else
+    hipLaunchKernelGGL((sample_sums_kernel<E, false, true>), grid, dim3(SS_THREADS), 0, s, logits, a);
+  const dim3 rows(static_cast<unsigned>(a.M));
+  if (a.scale > 0.0 && filters(a)) {
+    hipLaunchKernelGGL((sample_list_kernel<E>), grid, dim3(SS_THREADS), 0, s, logits, a);
+    hipLaunchKernelGGL((sample_kernel<E, true>), rows, dim3(SP_THREADS), 0, s, logits, a);
+  } else {
+    hipLaunchKernelGGL((sample_kernel<E, false>), rows, dim3(SP_THREADS), 0, s, logits, a);
+  }
+  return launch_status();
+}
 
 int launch_sample(const void* logits, int logits_type, const int32_t* rows, const int32_t* n_rows, int M, int V,
-                  const float* u, const reflex_sample_params& p, int T, int32_t* tokens, float* conf, void*,
+                  const float* u, const reflex_sample_params& p, int T, int32_t* tokens, float* conf, void* ws,
                   hipStream_t s) {
-  SampleArgs a{rows, n_rows, M, V, T, u, p.temperature > 0.0f ? SP_LOG2E / static_cast<double>(p.temperature) : 0.0,
-               p.min_p > 0.0f ? std::log2(static_cast<double>(p.min_p)) : -std::numeric_limits<double>::infinity(),
-               p.top_k > 0 && p.top_k < V ? p.top_k : V, static_cast<double>(p.top_p), tokens, conf};
-  if (logits_type == REFLEX_TYPE_F32)
-    hipLaunchKernelGGL(sample_kernel<float>, dim3(M), dim3(SP_THREADS), 0, s, static_cast<const float*>(logits), a);
-  else
-    hipLaunchKernelGGL(sample_kernel<uint16_t>, dim3(M), dim3(SP_THREADS), 0, s, static_cast<const uint16_t*>(logits), a);
-  return launch_status();
+  const SampleArgs a{rows, n_rows, M, V, T, parts_of(M, V), u,
+                     p.temperature > 0.0f ? SP_LOG2E / static_cast<double>(p.temperature) : 0.0,
+                     p.min_p > 0.0f ? std::log2(static_cast<double>(p.min_p)) : -std::numeric_limits<double>::infinity(),
+                     p.top_k > 0 && p.top_k < V ? p.top_k : V, static_cast<double>(p.top_p), tokens, conf,
+                     static_cast<Part*>(ws), reinterpret_cast<int32_t*>(static_cast<char*>(ws) + part_bytes(M, V)),
+                     reinterpret_cast<Listed*>(static_cast<char*>(ws) + part_bytes(M, V) + listed_bytes(M, V))};
+  return logits_type == REFLEX_TYPE_F32 ? launch_sample_as(static_cast<const float*>(logits), a, s)
+                                        : launch_sample_as(static_cast<const uint16_t*>(logits), a, s);
 }
 
 }  // namespace rfx
