@@ -13,12 +13,15 @@
 //     above it.  Groups of eight lanes leave their maxima, from which a bound for top-k follows.
 //  2. With filters: each part's elements above a bound that no kept logit lies below are listed, in
 //     index order, if they are few enough, as they mostly are.
-//  3. A workgroup of 16 waves a row.  Without filters it finds the part that u falls into and scans that
-//     one.  The last kept logit of top-k and top-p is found by counts or weights (fixed point, so that
-//     the sums do not depend on the order of the atomics) in 2048 bins, first linear ones between the
-//     bound and the maximum, then over the 32-bit order keys of one bin, on the list where there is one,
-//     else in passes over the row (in the memory-side cache by then), until what is left fits a list.
-//     The draw goes over the list, or over the row's sixteenths and a scan of one.
+//  3. A wave a row.  Without filters it finds the part that u falls into and scans that one.  With
+//     filters it holds the list in registers, finds the last kept logit of top-k and of top-p bit by
+//     bit of the 32-bit order keys (counts by ballots, weights in fixed point), and draws.
+//  4. With filters: a workgroup of 16 waves for each row whose list did not fit (flat rows, mostly of
+//     top-p).  The last kept logit is found by counts or weights in 2048 bins, first linear ones between
+//     the bound and the maximum, then over the order keys of one bin, in passes over the row (in the
+//     memory-side cache by then) until what is left fits a list in LDS.  (Fixed-point weights: the
+//     sums do not depend on the order of the atomics.)  The draw goes over the row's sixteenths and a
+//     scan of one.
 // Everything is inlined and in registers: no stack.
 #include <algorithm>
 #include <cmath>
@@ -35,7 +38,8 @@ constexpr int SP_THREADS = 1024, SP_WAVES = SP_THREADS / kWave;     // second la
 constexpr int SP_PARTS = 256;                                       // most parts of a row
 constexpr int SP_BIN_BITS = 11, SP_BINS = 1 << SP_BIN_BITS;
 constexpr int SP_LANE = 4, SP_SEG = SP_LANE * kWave;      // list entries of a lane and of a wave
-constexpr int SP_LIST = SP_WAVES * SP_SEG;
+constexpr int SL_LANE = 16, SL_MOST = SL_LANE * kWave;    // a row's list: entries of a lane, of all
+constexpr int SL_LIST = 4 * SL_MOST;                      // the parts' shares of it are larger
 constexpr int SP_SCAN = 8;                                // consecutive elements of a thread in a scan
 static_assert(SP_BINS == 2 * SP_THREADS && SP_PARTS <= SP_THREADS, "two bins a thread");
 constexpr double SP_LOG2E = 1.4426950408889634074;
@@ -51,7 +55,7 @@ struct Part {
   float group[8];      // maxima of the groups of eight lanes
 };
 
-// What the second launch leaves of a part: elements listed, or -1 for too many.
+// An element that the second launch lists.
 struct Listed {
   uint32_t key;
   int index;
@@ -68,10 +72,11 @@ struct SampleArgs {
   int32_t* tokens;
   float* conf;
   Part* part;            // [M, parts]
-  int32_t* listed;       // [M, parts]
+  int32_t* listed;       // [M, parts]: the parts' numbers of listed elements, -1 for too many
   Listed* list;          // [M, SP_LIST]: parts' shares one after the other
 };
 
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 constexpr double kMagic = 0x1.8p46;      // its last place is 1 / 64
 
 // a b + c as one instruction with a destination of its own.  (The compiler prefers the form that adds
@@ -96,10 +101,10 @@ RFX_DEVICE double pow2_entry(int j) {
 RFX_DEVICE void pow2_parts(double y, double r, const double* table, double& p, double& t) {
   const uint32_t n = static_cast<uint32_t>(__double_as_longlong(y));      // 64 x, rounded
   p = fma64(r, fma64(r, fma64(r, 0.05550410866482158, 0.24022650695910071), 0.69314718055994531), 1.0);
-  const uint64_t e = static_cast<uint64_t>(
-      __double_as_longlong(*reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + ((n << 3) & 0x1f8u))));
-  t = __longlong_as_double(static_cast<long long>(((static_cast<uint64_t>(static_cast<uint32_t>(e >> 32) + (n << 14))) << 32) |
-                                                  static_cast<uint32_t>(e)));
+  u32x2_t e = __builtin_bit_cast(
+      u32x2_t, *reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + ((n << 3) & 0x1f8u)));
+  e[1] += n << 14;
+  t = __builtin_bit_cast(double, e);
 }
 RFX_DEVICE double pow2_of(double y, double r, const double* table) {
   double p, t;
@@ -196,12 +201,17 @@ struct Row {
     const int steps = (end - begin + kWave - 1) / kWave;
     for (int st = part == 0 ? -1 : 0; st < steps + (part == parts - 1 ? 1 : 0); ++st) {
       if (WHOLE) {
-        while (st >= 0 && begin + (st + 1) * kWave <= end) {
-          const Values v = unpack(q0);
-          const int first = head + i * VEC;
-          next();
-          f(v, VEC, first, std::true_type{});
-          ++st;
+        auto whole = [&](uint4& q) SP_INLINE {      // (the four loads take turns: no copies between them)
+          const Values v = unpack(q);
+          q = load(i + 4 * kWave);
+          f(v, VEC, head + i * VEC, std::true_type{});
+          i += kWave;
+        };
+        for (; st >= 0 && begin + (st + 4) * kWave <= end; st += 4) {
+          whole(q0);
+          whole(q1);
+          whole(q2);
+          whole(q3);
         }
         if (st >= steps + (part == parts - 1 ? 1 : 0)) break;
       }
@@ -242,7 +252,7 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
   double sum = 0.0, flat = 0.0;
   row.template each<true>(part, [&](Values v, int n, int i, auto whole) SP_INLINE {
     constexpr bool WHOLE = decltype(whole)::value;
-    // (fmaxf passes NaN by; below, NaN and -inf become the lowest number, whose weight is nothing)
+    // (fmaxf passes NaN by)
     float m = fmaxf(v[0], SP_NONE);
 #pragma unroll
     for (int k = 1; k < VEC; ++k) m = fmaxf(m, v[k]);
@@ -262,10 +272,10 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
     float z = 0.0f;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      const float l = fmaxf(v[k], SP_LOWEST);
+      const float l = fmaxf(v[k], SP_LOWEST);      // (NaN and -inf too: the weight of that is nothing)
       if (DRAWS) {
         const double d = static_cast<double>(l) - static_cast<double>(ref);
-        const double y = fmax(fma(d, scale, kMagic), kMagic - 1020.0);
+        const double y = fmax(fma(d, scale, kMagic), kMagic - 1020.0);      // (below 2^-1020: next to nothing)
         double p, t;
         pow2_parts(y, fma(d, scale, kMagic - y), table, p, t);
         if (WHOLE)
@@ -314,7 +324,23 @@ RFX_DEVICE float filter_bound(const SampleArgs& a, const Part* part, double m, d
   const float top = static_cast<float>(m);
   const bool by_count = a.top_k < a.V, by_mass = a.top_p < 1.0;
   float cut = SP_LOWEST;
-  if (by_count && a.top_k <= groups) {
+  if (by_count && 2 * a.top_k <= a.parts) {      // (enough parts: their maxima do)
+    uint32_t bound = 0;
+    uint32_t key[SP_PARTS / kWave];
+#pragma unroll
+    for (int q = 0; q < SP_PARTS / kWave; ++q) {
+      const int p = q * kWave + lane;
+      key[q] = p < a.parts ? f32_order_key(part[p].top) : 0u;
+    }
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t t = bound | (1u << bit);
+      int n = 0;
+#pragma unroll
+      for (int q = 0; q < SP_PARTS / kWave; ++q) n += __popcll(__ballot(key[q] >= t));
+      if (n >= a.top_k) bound = t;
+    }
+    if (bound > f32_order_key(SP_LOWEST)) cut = f32_from_order_key(bound);
+  } else if (by_count && a.top_k <= groups) {
     uint32_t bound = 0;
     uint32_t key[8 * SP_PARTS / kWave];
 #pragma unroll
@@ -338,6 +364,15 @@ RFX_DEVICE float filter_bound(const SampleArgs& a, const Part* part, double m, d
   return fminf(fmaxf(cut - 1e-6f * fmaxf(fabsf(cut), fabsf(top)), SP_LOWEST), top);
 }
 
+// Weights in fixed point: times the power of two that brings the sum of all between 2^50 and 2^51, and
+// rounded.  (A power of two: equal logits at the maximum have weight 1 and borders that are exact.)
+RFX_DEVICE double fixed_scale(double total) {
+  return __longlong_as_double((2096ll - (__double_as_longlong(total) >> 52)) << 52);
+}
+RFX_DEVICE uint64_t fixed_point(double w, double scale) {
+  return static_cast<uint64_t>(__double_as_longlong(fma(w, scale, 0x1p52))) - 0x4330000000000000ull;
+}
+
 // A row's maximum and sum of weights from its parts, by one wave.
 RFX_DEVICE void row_sums(const SampleArgs& a, const Part* part, const double* table, float& top, double& total) {
   const int lane = threadIdx.x & 63;
@@ -355,22 +390,28 @@ __global__ __launch_bounds__(SS_THREADS) void sample_list_kernel(const E* __rest
   constexpr int VEC = Row<E>::VEC;
   using Values = typename Row<E>::Values;
   __shared__ double table[64];
+  __shared__ float s_cut;
   const int tid = threadIdx.x, lane = tid & 63;
   if (tid < 64) table[tid] = pow2_entry(tid);
   __syncthreads();
   const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + (tid >> 6));
-  const int j = item / a.parts, p = item - j * a.parts;
+  const int j = item / a.parts, p = item - j * a.parts;      // (one row a workgroup: parts % SS_WAVES = 0)
   if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
   const Part* const part = a.part + static_cast<size_t>(j) * a.parts;
-  float top;
-  double total;
-  row_sums(a, part, table, top, total);
-  int n_list = -1, room = SP_LIST / a.parts;
-  if (top > SP_NONE && top < -SP_NONE) {
-    const float cut = filter_bound(a, part, top, total);
-    Listed* const list = a.list + static_cast<size_t>(j) * SP_LIST + static_cast<size_t>(p) * room;
+  if (tid < kWave) {
+    float top;
+    double total;
+    row_sums(a, part, table, top, total);
+    const float cut = top > SP_NONE && top < -SP_NONE ? filter_bound(a, part, top, total) : -SP_NONE;
+    if (lane == 0) s_cut = cut;
+  }
+  __syncthreads();
+  const float cut = s_cut;      // (+inf: a row without weight, or with +inf: no list)
+  const int room = SL_LIST / a.parts;
+  int n_list = 0;      // (uniform in the wave)
+  if (cut < -SP_NONE) {
+    Listed* const list = a.list + static_cast<size_t>(j) * SL_LIST + static_cast<size_t>(p) * room;
     const Row<E> row(logits + static_cast<size_t>(j) * a.V, a.V, a.parts);
-    n_list = 0;      // (uniform in the wave)
     row.template each<false>(p, [&](Values v, int n, int i, auto) SP_INLINE {
       uint32_t on = 0;
 #pragma unroll
@@ -387,16 +428,301 @@ __global__ __launch_bounds__(SS_THREADS) void sample_list_kernel(const E* __rest
         }
       }
     });
-    if (n_list > room) n_list = -1;
   }
-  if (lane == 0) a.listed[static_cast<size_t>(j) * a.parts + p] = n_list;
+  if (lane == 0) a.listed[static_cast<size_t>(j) * a.parts + p] = n_list > room ? -1 : n_list;
+}
+
+// A row's sums from its parts', by one wave; first: the maximum's first index.
+RFX_DEVICE void row_flat(const SampleArgs& a, const Part* part, const double* table, float& top, int& first,
+                         double& total, double& flat) {
+  const int lane = threadIdx.x & 63;
+  uint64_t most = 0;
+  for (int p = lane; p < a.parts; p += kWave)
+    most = max(most, (static_cast<uint64_t>(f32_order_key(part[p].top)) << 32) | (0x7fffffffu - static_cast<uint32_t>(part[p].first)));
+  most = wave_max_u64(most);
+  top = f32_from_order_key(static_cast<uint32_t>(most >> 32));
+  first = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(most));
+  total = flat = 0.0;
+  for (int p = lane; p < a.parts; p += kWave) {
+    const double down = static_cast<double>(part[p].top) - static_cast<double>(top);
+    total += part[p].sum * pow2_or_0(down * a.scale, table);
+    flat += part[p].flat * pow2_or_0(down * SP_LOG2E, table);
+  }
+  total = wave_sum64(total);
+  flat = a.scale == SP_LOG2E ? total : wave_sum64(flat);
+}
+
+// Of the lanes' weights in lane order, the lane that `target` falls into, and what is left of it there;
+// else (the order of the additions) the last lane with weight, +inf; -1: none has weight.
+RFX_DEVICE int pick_lane(double w, double target, double before, double& rest, bool& hit) {
+  const double incl = wave_inclusive_scan64(w);
+  const uint64_t hits = __ballot(w > 0.0 && before + incl > target), any = __ballot(w > 0.0);
+  hit = hits != 0;
+  rest = hit ? target - (before + incl - w) : __builtin_huge_val();
+  return hit ? __builtin_ctzll(hits) : (any != 0 ? 63 - __builtin_clzll(any) : -1);
+}
+
+template <class E, bool FILTERS>
+__global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restrict__ logits, SampleArgs a) {
+  __shared__ double table[64];
+  __shared__ int s_at[SS_WAVES][SP_PARTS + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (tid < 64) table[tid] = pow2_entry(tid);
+  __syncthreads();
+  const int j = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + wv), V = a.V, parts = a.parts;
+  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
+  const int pos = a.rows == nullptr ? j : a.rows[j];
+  if (pos < 0 || pos >= a.T) return;
+  const Part* const part = a.part + static_cast<size_t>(j) * parts;
+  const Row<E> row(logits + static_cast<size_t>(j) * V, V, parts);
+  float top;
+  int token;
+  double total, flat;
+  row_flat(a, part, table, top, token, total, flat);
+  float u = a.u[pos];
+  u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+  const double m = top, scale = a.scale;
+  auto weight = [&](uint32_t k) SP_INLINE {
+    return pow2_or_0((static_cast<double>(f32_from_order_key(k)) - m) * scale, table);
+  };
+  if (top == SP_NONE) {            // nothing has weight
+    token = -1;
+    flat = 1.0;
+  } else if (top == -SP_NONE) {    // the +inf ones have the same weight each, the others none
+    int n = 0;
+    for (int i = lane; i < V; i += kWave) n += row.at(i) == top ? 1 : 0;
+    n = wave_sum_i32(n);
+    flat = n;
+    if (scale > 0.0) {
+      if (a.top_k < n) n = a.top_k;
+      if (a.top_p < 1.0) n = max(1, static_cast<int>(ceil(a.top_p * n)));
+      int want = min(static_cast<int>(u * static_cast<double>(n)), n - 1);      // the want-th of them
+      for (int i0 = 0; i0 < V; i0 += kWave) {
+        uint64_t on = __ballot(i0 + lane < V && row.at(min(i0 + lane, V - 1)) == top);
+        const int here = __popcll(on);
+        if (want < here) {
+          for (; want > 0; --want) on &= on - 1;
+          token = i0 + __builtin_ctzll(on);
+          break;
+        }
+        want -= here;
+      }
+    }
+  } else if (FILTERS) {
+    // the list, lane l's entries R l .. R l + R - 1 of it
+    const int32_t* const listed = a.listed + static_cast<size_t>(j) * parts;
+    int all = 0;
+    bool fits = true;
+    for (int p0 = 0; p0 < parts; p0 += kWave) {
+      const int n = p0 + lane < parts ? listed[p0 + lane] : 0;
+      fits = fits && __ballot(n < 0) == 0;
+      const int incl = wave_inclusive_scan_i32(n, lane);
+      if (p0 + lane < parts) s_at[wv][p0 + lane] = all + incl - n;
+      all += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (!fits || all > SL_MOST) return;      // the fourth launch's
+    if (lane == 0) s_at[wv][parts] = all;
+    __builtin_amdgcn_wave_barrier();
+    const int R = (all + kWave - 1) / kWave, room = SL_LIST / parts;
+    const Listed* const list = a.list + static_cast<size_t>(j) * SL_LIST;
+    uint32_t key[SL_LANE];
+    int index[SL_LANE];
+    {
+      int at = R * lane, p = 0;
+      for (int step = 128; step > 0; step >>= 1)      // the part that holds entry `at`
+        if (p + step < parts && s_at[wv][p + step] <= at) p += step;
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r) {
+        key[r] = 0;
+        index[r] = 0;
+        if (r < R && at < all) {
+          while (s_at[wv][p + 1] <= at) ++p;
+          const Listed l = list[static_cast<size_t>(p) * room + (at - s_at[wv][p])];
+          key[r] = l.key;
+          index[r] = l.index;
+          ++at;
+        }
+      }
+    }
+    // The border: keys above it are kept, and the first `ties` equal to it.  Keys are tried bit by bit
+    // from the first in which the listed ones differ.
+    const bool by_count = a.top_k < V, by_mass = a.top_p < 1.0;
+    const uint32_t key_top = f32_order_key(top);
+    uint32_t least = key[0] != 0 ? key[0] : key_top;
+#pragma unroll
+    for (int r = 1; r < SL_LANE; ++r) least = min(least, key[r] != 0 ? key[r] : key_top);
+    least = ~wave_max_u32(~least);
+    const int bits = least == key_top ? 0 : 32 - __builtin_clz(least ^ key_top);      // that differ
+    const uint32_t common = bits == 32 ? 0u : key_top >> bits << bits;
+    uint32_t border = 0;
+    int ties = 0x7fffffff;
+    if (by_count && a.top_k < all) {
+      border = common;
+      for (int bit = bits - 1; bit >= 0; --bit) {
+        const uint32_t t = border | (1u << bit);
+        if (t > key_top) continue;
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < SL_LANE; ++r)
+          if (r < R) n += __popcll(__ballot(key[r] >= t));
+        if (n >= a.top_k) border = t;
+      }
+      int above = 0;
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r)
+        if (r < R) above += __popcll(__ballot(key[r] > border));
+      ties = a.top_k - above;
+    }
+    // Of what is equal to `border`, this lane's first's rank.
+    auto tie_rank = [&]() SP_INLINE {
+      int n = 0;
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r) n += key[r] == border ? 1 : 0;
+      return wave_inclusive_scan_i32(n, lane) - n;
+    };
+    double w[SL_LANE];
+    {
+      int rank = tie_rank();
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r) {
+        const bool tie = key[r] == border;
+        w[r] = r < R && key[r] != 0 && (key[r] > border || (tie && rank < ties)) ? weight(key[r]) : 0.0;
+        rank += tie ? 1 : 0;
+      }
+    }
+    if (by_mass) {
+      const double fixed = fixed_scale(total);
+      uint64_t q[SL_LANE], sum = 0;
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r) {
+        q[r] = r < R ? fixed_point(w[r], fixed) : 0;
+        sum += q[r];
+      }
+      const double want = a.top_p * (by_count ? static_cast<double>(wave_sum64(sum)) : total * fixed);
+      uint32_t last = common;      // the largest key from which on the weights sum to `want`
+      for (int bit = bits - 1; bit >= 0; --bit) {
+        const uint32_t t = last | (1u << bit);
+        if (t > key_top) continue;
+        sum = 0;
+#pragma unroll
+        for (int r = 0; r < SL_LANE; ++r)
+          if (r < R) sum += key[r] >= t ? q[r] : 0;
+        if (static_cast<double>(wave_sum64(sum)) >= want) last = t;
+      }
+      uint64_t above = 0;
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r) above += key[r] > last ? q[r] : 0;
+      above = wave_sum64(above);
+      const double each = static_cast<double>(fixed_point(weight(last), fixed));
+      border = last;      // (below all keys: all are needed)
+      ties = each > 0.0 ? max(1, static_cast<int>(fmin(ceil((want - static_cast<double>(above)) / each), 2e9))) : 0;
+      int rank = tie_rank();
+#pragma unroll
+      for (int r = 0; r < SL_LANE; ++r) {
+        const bool tie = key[r] == border;
+        if (!(key[r] > border || (tie && rank < ties))) w[r] = 0.0;
+        rank += tie ? 1 : 0;
+      }
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int r = 0; r < SL_LANE; ++r) {
+      if (r < R) {
+        if ((static_cast<double>(f32_from_order_key(key[r])) - m) * scale < a.floor2) w[r] = 0.0;
+        sum += w[r];
+      }
+    }
+    double rest;
+    bool hit;
+    const int lane_of = pick_lane(sum, u * wave_sum64(sum), 0.0, rest, hit);
+    double cum = 0.0;
+    int mine = -1;
+    bool past = false;
+    rest = lane == lane_of ? rest : 0.0;
+#pragma unroll
+    for (int r = 0; r < SL_LANE; ++r) {
+      if (r < R && w[r] > 0.0 && !past) {
+        cum += w[r];
+        mine = index[r];
+        past = cum > rest;
+      }
+    }
+    if (lane_of >= 0) token = __builtin_amdgcn_readlane(mine, lane_of);
+  } else if (scale > 0.0) {
+    // the part that u falls into, 64 parts at a time, then its elements, eight consecutive ones a lane
+    double target = u * total, before = 0.0, rest = 0.0;
+    int last_part = 0;
+    for (int p0 = 0; p0 < parts; p0 += kWave) {
+      const double w = p0 + lane < parts ? part[p0 + lane].sum * pow2_or_0((static_cast<double>(part[p0 + lane].top) - m) * scale, table) : 0.0;
+      bool hit;
+      double left;
+      const int lane_of = pick_lane(w, target, before, left, hit);
+      before += wave_sum64(w);
+      if (lane_of >= 0) {
+        last_part = p0 + lane_of;
+        const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(left));
+        rest = __longlong_as_double(static_cast<long long>(
+            (static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(bits >> 32), lane_of))) << 32) |
+            static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(bits), lane_of))));
+      }
+      if (hit) break;
+    }
+    const int begin = row.begin(last_part), end = row.begin(last_part + 1);
+    uint32_t next[SP_SCAN];
+    auto load = [&](int i0) SP_INLINE {
+#pragma unroll
+      for (int e = 0; e < SP_SCAN; ++e) {
+        const int i = i0 + SP_SCAN * lane + e;
+        next[e] = i < end ? f32_order_key(fmaxf(row.at(i), SP_NONE)) : 0u;
+      }
+    };
+    before = 0.0;
+    load(begin);
+    for (int i0 = begin; i0 < end; i0 += SP_SCAN * kWave) {
+      double w[SP_SCAN], sum = 0.0;
+#pragma unroll
+      for (int e = 0; e < SP_SCAN; ++e) {
+        w[e] = next[e] > f32_order_key(SP_NONE) ? weight(next[e]) : 0.0;
+        sum += w[e];
+      }
+      load(i0 + SP_SCAN * kWave);
+      bool hit;
+      double left;
+      const int lane_of = pick_lane(sum, rest, before, left, hit);
+      before += wave_sum64(sum);
+      double cum = 0.0;
+      int mine = -1;
+      bool past = false;
+#pragma unroll
+      for (int e = 0; e < SP_SCAN; ++e) {
+        if (w[e] > 0.0 && !past) {
+          cum += w[e];
+          mine = i0 + SP_SCAN * lane + e;
+          past = cum > left;
+        }
+      }
+      if (lane_of >= 0) token = __builtin_amdgcn_readlane(mine, lane_of);
+      if (hit) break;
+    }
+  }
+  if (lane == 0) {
+    a.tokens[pos] = token;
+    if (a.conf != nullptr) {
+      double w = 0.0;
+      if (token >= 0) {
+        const float l = row.at(token);
+        w = l == top ? 1.0 : pow2_or_0((static_cast<double>(l) - m) * SP_LOG2E, table);
+      }
+      a.conf[pos] = static_cast<float>(w / flat);
+    }
+  }
 }
 
 struct SampleShared {
   double table[64];
-  double sum[SP_WAVES], flat[SP_WAVES], part_sum[SP_PARTS];
-  uint64_t best[SP_WAVES], wave_mass[SP_WAVES];
-  int wave_count[SP_WAVES], ties[SP_WAVES], seg_n[SP_WAVES], part_at[SP_PARTS];
+  double sum[SP_WAVES];
+  uint64_t wave_mass[SP_WAVES];
+  int wave_count[SP_WAVES], ties[SP_WAVES], seg_n[SP_WAVES];
   uint32_t first[SP_WAVES], last[SP_WAVES];
   double target;
   uint64_t above;
@@ -407,77 +733,38 @@ struct SampleShared {
   int index[SP_WAVES][SP_SEG];
 };
 
-template <class E, bool FILTERS>
-__global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict__ logits, SampleArgs a) {
+template <class E>
+__global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __restrict__ logits, SampleArgs a) {
   constexpr int VEC = Row<E>::VEC;
   using Values = typename Row<E>::Values;
   __shared__ SampleShared s;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = blockIdx.x, V = a.V, parts = a.parts;
   const double scale = a.scale, least = a.floor2;
-  const int used = a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M);
-  if (j >= used) return;
+  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
   const int pos = a.rows == nullptr ? j : a.rows[j];
   if (pos < 0 || pos >= a.T) return;
+  bool fits = true;
+  int all = 0;
+  for (int p0 = 0; p0 < parts; p0 += kWave) {
+    const int n = p0 + lane < parts ? a.listed[static_cast<size_t>(j) * parts + p0 + lane] : 0;
+    fits = fits && __ballot(n < 0) == 0;
+    all += wave_sum_i32(n);
+  }
+  if (fits && all <= SL_MOST) return;      // the third launch's
   if (tid < 64) s.table[tid] = pow2_entry(tid);
-  const Row<E> row(logits + static_cast<size_t>(j) * V, V, SP_WAVES);      // (a wave a sixteenth)
-  const bool draws = scale > 0.0;
-
-  // ---- the row's maximum and sums from its parts'
-  const Part* const part_of = a.part + static_cast<size_t>(j) * parts;
-  Part mine{0.0, 0.0, SP_NONE, 0x7fffffff, {}};
-  if (tid < parts) {
-    mine.sum = part_of[tid].sum;
-    mine.flat = part_of[tid].flat;
-    mine.top = part_of[tid].top;
-    mine.first = part_of[tid].first;
-  }
-  const uint64_t key = wave_max_u64((static_cast<uint64_t>(f32_order_key(mine.top)) << 32) |
-                                    (0x7fffffffu - static_cast<uint32_t>(mine.first)));
-  if (lane == 0) s.best[wv] = key;
   __syncthreads();
-  const uint64_t most = wave_max_u64(lane < SP_WAVES ? s.best[lane] : 0);
-  const uint32_t key_top = static_cast<uint32_t>(most >> 32);
-  const float top = f32_from_order_key(key_top);
-  if (top == SP_NONE) {        // nothing has weight
-    if (tid == 0) {
-      a.tokens[pos] = -1;
-      if (a.conf != nullptr) a.conf[pos] = 0.0f;
-    }
-    return;
-  }
+  const Part* const part_of = a.part + static_cast<size_t>(j) * parts;
+  const Row<E> row(logits + static_cast<size_t>(j) * V, V, SP_WAVES);      // (a wave a sixteenth)
+  float top;
+  int token;
+  double total, flat;
+  row_flat(a, part_of, s.table, top, token, total, flat);
   const double m = top;
-  const bool inf_row = top == -SP_NONE;      // the +inf ones have weight 1, the others none
-  // Powers of two of logits by their keys.
-  auto power = [&](uint32_t k) SP_INLINE {
-    if (inf_row) return k == key_top ? 0.0 : -__builtin_huge_val();
-    return (static_cast<double>(f32_from_order_key(k)) - m) * scale;
-  };
+  const uint32_t key_top = f32_order_key(top);
+  auto power = [&](uint32_t k) SP_INLINE { return (static_cast<double>(f32_from_order_key(k)) - m) * scale; };
   auto key_of = [&](float l) SP_INLINE { return f32_order_key(fmaxf(l, SP_NONE)); };      // (NaN as -inf)
   auto weight = [&](uint32_t k) SP_INLINE { return pow2_or_0(power(k), s.table); };
-  double total, flat;
-  if (inf_row) {
-    double n = 0.0;
-    row.template each<false>(wv, [&](Values v, int count, int, auto) SP_INLINE {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) n += e < count && v[e] == -SP_NONE ? 1.0 : 0.0;
-    });
-    total = flat = wave_sum64(n);
-  } else {
-    const double down = static_cast<double>(mine.top) - m;
-    const double sum = mine.sum * pow2_or_0(down * scale, s.table);
-    if (tid < parts) s.part_sum[tid] = sum;
-    total = wave_sum64(sum);
-    flat = scale == SP_LOG2E ? total : wave_sum64(mine.flat * pow2_or_0(down * SP_LOG2E, s.table));
-  }
-  if (lane == 0) {
-    s.sum[wv] = total;
-    s.flat[wv] = flat;
-  }
-  __syncthreads();
-  waves_before(s.sum, 0, total);
-  waves_before(s.flat, 0, flat);
-  __syncthreads();
 
   // Of the threads' weights in thread order, the thread that `target` (of_all: times the sum) falls
   // into: s.target is then what is left of it; else the last thread with weight, s.target inf; -1: none
@@ -502,42 +789,34 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
     __syncthreads();
     return winner;
   };
-  int token = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(most));
-  if (draws) {
+  {
     float u = a.u[pos];
     u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
     // ---- filters: keys above `border` are kept, and the first `border_ties` of those equal to it; of
     // both only those with power() >= least
     const bool by_count = a.top_k < V, by_mass = a.top_p < 1.0;
-    const bool some = FILTERS || inf_row;
     uint32_t border = f32_order_key(SP_NONE);
     int border_ties = 0;
     bool listed = false;      // the list holds all elements that may be kept
     double sum_above = 0.0;   // kept weights of this wave's sixteenth above the elements on the list,
     bool summed = false;      // which are all that may be the border
-    if (!FILTERS && inf_row) border = key_top - 1;
-    if constexpr (FILTERS) {
-      const float cut = inf_row ? top : filter_bound(a, part_of, m, total);
+    {
+      const float cut = filter_bound(a, part_of, m, total);
       const uint32_t key_low = f32_order_key(cut);
       // Bins of the first pass: linear in the logit, bin 0 at the cut (so that more is higher), or at
       // weights of 2^-64, where the lower ones are in it too.
       const float range = fminf(top - cut, static_cast<float>(64.0 / scale));
       const float inv = range > 1e-30f ? (SP_BINS - 0.5f) / range : 0.0f;
       auto linear_bin = [&](float l) SP_INLINE {
-        const float t = inf_row ? 0.0f : (top - l) * inv;
-        return SP_BINS - 1 - static_cast<int>(fminf(t, SP_BINS - 1.0f));
+        return SP_BINS - 1 - static_cast<int>(fminf((top - l) * inv, SP_BINS - 1.0f));
       };
-      // Weights in fixed point, all together between 2^50 and 2^51.  (By a power of two: equal logits at
-      // the maximum have weight 1 and borders that are exact.)
-      const double fixed = __longlong_as_double((2096ll - (__double_as_longlong(total) >> 52)) << 52);
-      auto fixed_weight = [&](uint32_t k) SP_INLINE {
-        return static_cast<uint64_t>(__double_as_longlong(fma(weight(k), fixed, 0x1p52))) - 0x4330000000000000ull;
-      };
+      const double fixed = fixed_scale(total);
+      auto fixed_weight = [&](uint32_t k) SP_INLINE { return fixed_point(weight(k), fixed); };
       enum { LINEAR, KEYS, LIST };
       int stage = by_count || by_mass ? LINEAR : LIST;
       int within = -1, shift = 0;
       uint32_t lo = key_low, hi = key_top;
-      bool weigh = !by_count, have = listed;      // have: the list holds them all
+      bool weigh = !by_count, have = false;      // have: the list holds them all
       auto add = [&](uint32_t k, float l) SP_INLINE {
         const uint32_t bin = stage == LINEAR ? linear_bin(l) : (k - lo) >> shift;
         atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin]),
@@ -637,16 +916,15 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
         return want;
       };
       // Top-k, then top-p of what it leaves: a linear pass, then passes over the keys of its bin, each
-      // over the row until what is left fits the list.  What top-k leaves is listed if it fits; top-p
-      // alone works on with the first pass's list if that fits, min-p alone (and rows with +inf without
-      // top-k and top-p) needs nothing but such a list.
+      // over the row until what is left fits the list.  What top-k leaves is listed if it fits.  Min-p
+      // alone needs no pass.
       uint32_t from = key_low;      // elements below are cut off, of those equal to it all but `room`
       int room = 0x7fffffff;
       uint64_t above = 0, less = 0;
       double want = by_count ? static_cast<double>(a.top_k) : a.top_p * (total * fixed);
-      double share = inf_row && !by_count ? a.top_p : 0.0;
+      double share = 0.0;
       if (stage == LIST) border = key_low - 1;
-      for (;;) {
+      while (by_count || by_mass) {
         if (stage == KEYS) {
           const uint32_t span = hi - lo;
           const int bits = span == 0 ? 0 : 32 - __builtin_clz(span);
@@ -729,7 +1007,7 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
     double w[SP_LANE];
     double sum = 0.0;
     int ties_kept = 0;
-    if (FILTERS && (listed || summed)) {
+    if (listed || summed) {
       const int n = s.seg_n[wv];
       uint32_t k[SP_LANE];
       int ties = 0, all;
@@ -749,7 +1027,7 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
         sum += w[e];
       }
     }
-    if (FILTERS && listed) {
+    if (listed) {
       double sum_all;
       bool hit;
       const int winner = pick(sum, u, true, sum_all, hit);
@@ -773,11 +1051,11 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
       int part, begin, end, tie_room = 0;
       double unused;
       bool hit;
-      if (FILTERS && summed) {
+      if (summed) {
         sum = wave_sum64(sum + sum_above);
         ties_kept = wave_sum_i32(ties_kept);
         if (lane == 0) s.ties[wv] = ties_kept;
-      } else if (some) {
+      } else {
         int ties = 0;
         row.template each<false>(wv, [&](Values v, int n, int, auto) SP_INLINE {
 #pragma unroll
@@ -797,17 +1075,10 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
         __syncthreads();
         if (lane == 0) s.ties[wv] = mine_kept;
       }
-      if (some) {
-        part = pick(lane == 0 ? sum : 0.0, u, true, unused, hit) / kWave;      // (-1 / 64 is 0: weights are there)
-        tie_room = s.ties[part];
-        begin = row.begin(part);
-        end = row.begin(part + 1);
-      } else {
-        const Row<E> first(row.p, V, parts);
-        part = max(pick(tid < parts ? s.part_sum[tid] : 0.0, u, true, unused, hit), 0);
-        begin = first.begin(part);
-        end = first.begin(part + 1);
-      }
+      part = pick(lane == 0 ? sum : 0.0, u, true, unused, hit) / kWave;      // (-1 / 64 is 0: weights are there)
+      tie_room = s.ties[part];
+      begin = row.begin(part);
+      end = row.begin(part + 1);
       // that part, eight consecutive elements a thread; the last kept token stands in where the order
       // of the additions leaves the target at the part's end
       double target = s.target;
@@ -823,13 +1094,12 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
           ties += k[e] == border ? 1 : 0;
         }
         int rank = 0;
-        if (some) rank = tie_base + tie_rank(ties, all);
+        rank = tie_base + tie_rank(ties, all);
         double w[SP_SCAN], sum = 0.0;
 #pragma unroll
         for (int e = 0; e < SP_SCAN; ++e) {
           const bool tie = k[e] == border;
-          const bool keep = some ? kept(k[e], tie && rank < tie_room) : k[e] > f32_order_key(SP_NONE);
-          w[e] = keep ? weight(k[e]) : 0.0;
+          w[e] = kept(k[e], tie && rank < tie_room) ? weight(k[e]) : 0.0;
           rank += tie ? 1 : 0;
           sum += w[e];
         }
@@ -861,19 +1131,18 @@ __global__ __launch_bounds__(SP_THREADS) void sample_kernel(const E* __restrict_
   if (tid == 0) {
     a.tokens[pos] = token;
     if (a.conf != nullptr) {
-      const uint32_t k = key_of(row.at(token));
-      const double x = k == key_top ? 0.0 : (static_cast<double>(f32_from_order_key(k)) - m) * SP_LOG2E;
+      const double x = (static_cast<double>(row.at(token)) - m) * SP_LOG2E;
       a.conf[pos] = static_cast<float>(pow2_or_0(x, s.table) / flat);
     }
   }
 }
 
-// Parts of a row: 8192 elements at most (a scan's reach), more parts for few rows: a wave each, 4096
-// waves fill the GPU, but not fewer than two vectors a lane.
+// Parts of a row, a wave each: 4096 elements at most (the third launch scans one), more parts for few
+// rows (4096 waves fill the GPU, but not for fewer than 512 elements); a multiple of a workgroup's waves.
 int parts_of(int M, int V) {
-  const int least = (V + SP_SCAN * SP_THREADS - 1) / (SP_SCAN * SP_THREADS);
-  const int fill = std::min((4096 + M - 1) / std::max(M, 1), V / (2 * kWave * 4));
-  return std::min(std::max({least, fill, 1}), SP_PARTS);
+  const int least = (V + 4095) / 4096;
+  const int fill = std::min((4096 + M - 1) / std::max(M, 1), V / 512);
+  return std::min((std::max({least, fill, 1}) + SS_WAVES - 1) / SS_WAVES * SS_WAVES, SP_PARTS);
 }
 
 }  // namespace
@@ -884,7 +1153,7 @@ static bool filters(const SampleArgs& a) { return a.top_k < a.V || a.top_p < 1.0
 static size_t part_bytes(int M, int V) { return align_up(sizeof(Part) * static_cast<size_t>(M) * parts_of(M, V)); }
 static size_t listed_bytes(int M, int V) { return align_up(sizeof(int32_t) * static_cast<size_t>(M) * parts_of(M, V)); }
 size_t sample_ws_bytes(int M, int V) {
-  return part_bytes(M, V) + listed_bytes(M, V) + align_up(sizeof(Listed) * static_cast<size_t>(M) * SP_LIST);
+  return part_bytes(M, V) + listed_bytes(M, V) + align_up(sizeof(Listed) * static_cast<size_t>(M) * SL_LIST);
 }
 
 template <class E>
@@ -896,12 +1165,13 @@ static int launch_sample_as(const E* logits, const SampleArgs& a, hipStream_t s)
     hipLaunchKernelGGL((sample_sums_kernel<E, true, true>), grid, dim3(SS_THREADS), 0, s, logits, a);
   else
     hipLaunchKernelGGL((sample_sums_kernel<E, false, true>), grid, dim3(SS_THREADS), 0, s, logits, a);
-  const dim3 rows(static_cast<unsigned>(a.M));
+  const dim3 rows(static_cast<unsigned>((a.M + SS_WAVES - 1) / SS_WAVES));
   if (a.scale > 0.0 && filters(a)) {
     hipLaunchKernelGGL((sample_list_kernel<E>), grid, dim3(SS_THREADS), 0, s, logits, a);
-    hipLaunchKernelGGL((sample_kernel<E, true>), rows, dim3(SP_THREADS), 0, s, logits, a);
+    hipLaunchKernelGGL((sample_row_kernel<E, true>), rows, dim3(SS_THREADS), 0, s, logits, a);
+    hipLaunchKernelGGL((sample_flat_kernel<E>), dim3(static_cast<unsigned>(a.M)), dim3(SP_THREADS), 0, s, logits, a);
   } else {
-    hipLaunchKernelGGL((sample_kernel<E, false>), rows, dim3(SP_THREADS), 0, s, logits, a);
+    hipLaunchKernelGGL((sample_row_kernel<E, false>), rows, dim3(SS_THREADS), 0, s, logits, a);
   }
   return launch_status();
 }
