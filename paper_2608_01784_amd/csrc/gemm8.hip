@@ -45,6 +45,7 @@ namespace rfx {
 
 namespace {
 
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -57,7 +58,7 @@ constexpr int G8_XCDS = 8;
 constexpr int G8_BK = F8_BLOCK;                  // bytes of a slice's row
 constexpr int G8_CHUNKS = G8_BK / 16;
 constexpr int G8_OP_ROWS = 64 / G8_CHUNKS;       // rows of one wave's copy (1 KB)
-constexpr int G8_NJ = 2;                         // 32-row weight blocks per wave
+constexpr int G8_NJ = 4;                         // 32-row weight blocks per wave
 enum Mode { UP, DOWN, PLAIN };
 
 // s_waitcnt vmcnt(N) with expcnt and lgkmcnt left at their maxima (vmcnt in bits [3:0] and
@@ -94,68 +95,117 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)) * u;
 }
 
-// Staging of a wave's 32 x 32 output block: row pitch 80 bytes.
-constexpr int G8_STAGE_LD = 80, G8_STAGE = 32 * G8_STAGE_LD;
+// ---- epilogue stores of a plain tile ---------------------------------------------------------
+// A wave has 32 rows x 128 columns of a pair block as four accumulators of 32 columns: lane l, register r
+// holds row l % 32 and column 8 (r/4) + 4 (l/32) + r%4.  Rows go through the wave's 4 KB of scratch in
+// LDS, 128 bytes of each at a time (64 bf16 or 32 fp32 columns), and come back with neighbouring lanes
+// on neighbouring columns, so that a store writes whole 128-byte pieces of rows.  Chunk c (16 bytes) of row r
+// lies at c ^ (r % 8), free of bank conflicts both ways.  (Inline assembly: the compiler cannot tell
+// the scratch from the ring that copies in flight write, and would wait for those.)
+constexpr int G8_STAGE = 32 * 128;
 
-// Epilogue of one 32 x 32 block: rows row_base .., columns col_base .. of `out`, one bf16
-// rounding.  Lane l, register r holds row l % 32 and column 8 (r/4) + 4 (l/32) + r%4; the block
-// goes through the wave's staging buffer and comes back with 4 lanes per row, so a store writes 16
-// rows of 64 contiguous bytes.  N is a multiple of 8 here.  (Inline assembly: the compiler cannot
-// tell the buffer from the ring that copies in flight write, and would wait for those.)
-__device__ __forceinline__ void store_bf16(const f32x16_t& v, int row_base, int col_base, int row_end, int N,
-                                           uint16_t* __restrict__ out, uint32_t stage) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t wr = stage + (lane & 31) * G8_STAGE_LD + 8 * (lane >> 5);
-  const uint32_t rd = stage + (lane >> 2) * G8_STAGE_LD + 16 * (lane & 3);
-  u32x2_t p[4];
-#pragma unroll
-  for (int g = 0; g < 4; ++g) p[g] = u32x2_t{pack_bf16x2(v[4 * g], v[4 * g + 1]), pack_bf16x2(v[4 * g + 2], v[4 * g + 3])};
-  u32x4_t r0, r1;
-  asm volatile(
-      "ds_write_b64 %2, %4\n\t"
-      "ds_write_b64 %2, %5 offset:16\n\t"
-      "ds_write_b64 %2, %6 offset:32\n\t"
-      "ds_write_b64 %2, %7 offset:48\n\t"
-      "ds_read_b128 %0, %3\n\t"
-      "ds_read_b128 %1, %3 offset:1280\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r0), "=&v"(r1)
-      : "v"(wr), "v"(rd), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3])
-      : "memory");
-  const int row = row_base + (lane >> 2), col = col_base + 8 * (lane & 3);
-  if (col < N) {
-    if (row < row_end) *reinterpret_cast<u32x4_t*>(out + static_cast<size_t>(row) * N + col) = r0;
-    if (row + 16 < row_end) *reinterpret_cast<u32x4_t*>(out + static_cast<size_t>(row + 16) * N + col) = r1;
-  }
+__device__ __forceinline__ void lds_write64(uint32_t at, uint32_t a, uint32_t b) {
+  asm volatile("ds_write_b64 %0, %1" ::"v"(at), "v"(u32x2_t{a, b}) : "memory");
+}
+__device__ __forceinline__ void lds_write128(uint32_t at, float a, float b, float c, float d) {
+  asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(f32x4_t{a, b, c, d}) : "memory");
+}
+__device__ __forceinline__ uint32_t stage_at(uint32_t stage, int row, int chunk) {
+  return stage + row * 128 + ((chunk ^ (row & 7)) * 16);
 }
 
-// The same for any N and fp32 or bf16 rows, element by element.
-template <class OUT>
-__device__ __forceinline__ void store_any(const f32x16_t& v, int row_base, int col_base, int row_end, int N,
-                                          OUT* __restrict__ out) {
-  const int lane = threadIdx.x & 63, row = row_base + (lane & 31);
-  if (row >= row_end) return;
-  OUT* const to = out + static_cast<size_t>(row) * N;
+// The staged 32 rows x (128 / sizeof(OUT)) columns to `out`: rows row_base .. below row_end, columns
+// col_base .. below N.
+template <class OUT, bool ANY_N>
+__device__ __forceinline__ void store_staged(int row_base, int col_base, int row_end, int N, OUT* __restrict__ out,
+                                             uint32_t stage) {
+  constexpr int COLS = 128 / sizeof(OUT), VEC = 16 / sizeof(OUT);
+  const int lane = threadIdx.x & 63;
+  if (!ANY_N || N % VEC == 0) {      // whole vectors: 8 lanes a row
+    u32x4_t v[4];
+    uint32_t at[4];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int col = col_base + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-    if (col < N) {
-      if constexpr (sizeof(OUT) == 4)
-        to[col] = v[r];
-      else
-        to[col] = f32_to_bf16(v[r]);
+    for (int q = 0; q < 4; ++q) at[q] = stage_at(stage, (lane >> 3) + 8 * q, lane & 7);
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+        : "memory");
+    const int col = col_base + VEC * (lane & 7);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = row_base + (lane >> 3) + 8 * q;
+      if (row < row_end && col < N) *reinterpret_cast<u32x4_t*>(out + static_cast<size_t>(row) * N + col) = v[q];
+    }
+    return;
+  }
+  if constexpr (sizeof(OUT) == 4) {      // dwords: 32 lanes a row
+#pragma unroll 1
+    for (int q = 0; q < 16; q += 4) {
+      uint32_t v[4], at[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) at[e] = stage_at(stage, (lane >> 5) + 2 * (q + e), (lane & 31) / 4) + 4 * (lane & 3);
+      asm volatile(
+          "ds_read_b32 %0, %4\n\tds_read_b32 %1, %5\n\tds_read_b32 %2, %6\n\tds_read_b32 %3, %7\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+          : "memory");
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = row_base + (lane >> 5) + 2 * (q + e), col = col_base + (lane & 31);
+        if (row < row_end && col < N) out[static_cast<size_t>(row) * N + col] = __uint_as_float(v[e]);
+      }
+    }
+  } else {
+    // Any N: 32 lanes a row, two columns each as a dword where its address allows: in a row that starts at
+    // an odd element the pairs are columns 1-2, 3-4, .., and lane 31 has the first and the last column.
+#pragma unroll 1
+    for (int q = 0; q < 16; q += 2) {
+      uint32_t v[4], at[4];
+      int first[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = (lane >> 5) + 2 * (q + e), l = lane & 31;
+        const bool odd = ((static_cast<size_t>(row_base + r) * N + col_base) & 1) != 0;
+        first[e] = 2 * l + (odd ? 1 : 0);
+        const int c0 = first[e], c1 = (c0 + 1) % COLS;      // (odd, l = 31: columns 63 and 0)
+        at[2 * e] = stage_at(stage, r, c0 / 8) + 2 * (c0 % 8);
+        at[2 * e + 1] = stage_at(stage, r, c1 / 8) + 2 * (c1 % 8);
+      }
+      asm volatile(
+          "ds_read_u16 %0, %4\n\tds_read_u16 %1, %5\n\tds_read_u16 %2, %6\n\tds_read_u16 %3, %7\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+          : "memory");
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int row = row_base + (lane >> 5) + 2 * (q + e), c0 = col_base + first[e];
+        if (row >= row_end) continue;
+        OUT* const to = out + static_cast<size_t>(row) * N;
+        if (first[e] + 1 < COLS && c0 + 1 < N) {
+          *reinterpret_cast<uint32_t*>(to + c0) = v[2 * e] | (v[2 * e + 1] << 16);
+        } else {
+          if (c0 < N) to[c0] = static_cast<OUT>(v[2 * e]);
+          if (first[e] + 1 >= COLS && col_base < N) to[col_base] = static_cast<OUT>(v[2 * e + 1]);
+        }
+      }
     }
   }
 }
 
-// A tile shape: WM x WN waves, MI 32-row pair blocks by 64 weight rows each (wave (wm, wn) has
-// the pair blocks wm, wm + WM, ..: an expert's last tile then shortens all waves alike); rings of
-// A_SLOTS input-row and B_SLOTS weight slices, copied A_SLOTS - 1 and B_SLOTS - 1 steps ahead.
-template <int MI_, int WM_, int WN_, int A_SLOTS_, int B_SLOTS_>
+// A tile shape: 2 x 2 waves, one a SIMD, MI 32-row pair blocks by 128 weight rows each (wave (wm, wn) has
+// the pair blocks wm, wm + 2, ..: an expert's last tile then shortens all waves alike); rings of
+// A_SLOTS input-row and B_SLOTS weight slices, copied A_SLOTS - 1 and B_SLOTS - 1 steps ahead.  (Blocks of
+// 128 x 128 a wave read half as much LDS per product as eight waves' of 128 x 64, whose reads and copies
+// alone would take all of the LDS's rate.)
+template <int MI_, int A_SLOTS_, int B_SLOTS_>
 struct Shape8 {
-  static constexpr int MI = MI_, WM = WM_, WN = WN_, WAVES = WM_ * WN_, A_SLOTS = A_SLOTS_, B_SLOTS = B_SLOTS_;
+  static constexpr int MI = MI_, WM = 2, WN = 2, WAVES = 4, A_SLOTS = A_SLOTS_, B_SLOTS = B_SLOTS_;
   static constexpr int THREADS = 64 * WAVES;
-  static constexpr int BM = 32 * MI * WM, BROWS = 64 * WN;              // pair and weight rows of a tile
+  static constexpr int BM = 32 * MI * WM, BROWS = 32 * G8_NJ * WN;      // pair and weight rows of a tile
   static constexpr int A_BYTES = BM * G8_BK, B_BYTES = BROWS * G8_BK;   // one slice
   static constexpr int A_OPS = BM / G8_OP_ROWS / WAVES, B_OPS = BROWS / G8_OP_ROWS / WAVES;   // a wave's copies
   static constexpr int B_WROWS = BROWS / WAVES;                         // weight rows a wave copies
@@ -165,9 +215,8 @@ struct Shape8 {
   static constexpr int IN_FLIGHT = (B_SLOTS > A_SLOTS ? B_OPS : 0) + (A_SLOTS - 2) * (A_OPS + B_OPS);
   static_assert(A_SLOTS >= 2 && B_SLOTS >= A_SLOTS, "shape");
   static_assert(A_OPS * G8_OP_ROWS * WAVES == BM && B_OPS * G8_OP_ROWS * WAVES == BROWS, "whole copies");
-  static_assert(B_WROWS == 32, "a wave's weight rows are all gate or all up rows");
-  static_assert(WAVES * G8_STAGE <= B_BYTES && 16 * BM <= B_BYTES, "the epilogue's scratch fits a weight slot");
-  static_assert(BROWS == 2 * F8_BLOCK, "UP: a tile holds whole activation blocks");
+  static_assert(WAVES * G8_STAGE <= B_BYTES && 8 * BM <= B_BYTES, "the epilogue's scratch fits a weight slot");
+  static_assert(BROWS == 2 * F8_BLOCK && B_WROWS == F8_BLOCK / 2, "UP: half of the waves copy gate rows, half up rows");
   static_assert(4 * (REFLEX_MAX_EXPERTS + 1) <= LDS, "start-up scratch in the rings");
   static_assert(LDS <= 160 * 1024 && IN_FLIGHT < 64, "LDS and vmcnt range");
 };
@@ -191,7 +240,7 @@ struct Args8 {
 // BIG: x of 2^31 bytes or more, addressed with 64-bit pointers (a buffer resource's byte offset
 // has 32 bits, of which the upper half is kept for skipped copies).
 template <Mode MODE, class S, bool BIG, class OUT>
-__global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
+__global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   constexpr int MI = S::MI, A_OPS = S::A_OPS, B_OPS = S::B_OPS;
   constexpr bool WIDE = MODE == PLAIN && sizeof(OUT) == 4;       // fp32 results
   constexpr int BN = MODE == UP ? S::BROWS / 2 : S::BROWS;       // output columns of a tile
@@ -288,11 +337,15 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
   const bool short_k = nk < S::B_SLOTS;
   auto lane_row = [&](int q) { return q * G8_OP_ROWS + lane / G8_CHUNKS; };
   auto lane_chunk = [&](int q) { return ((lane % G8_CHUNKS) ^ ((lane_row(q) / 2) % G8_CHUNKS)) * 16; };
-  using Off = typename std::conditional<BIG, size_t, uint32_t>::type;
-  int a_tile = -1, a_k = nk, a_rot = 0, a_ops = 0, na_rot = 0, na_ops = 0;
+  // Gathered rows (UP) have an offset a copy; contiguous ones a first row, copies j and j + 2 being 16 rows
+  // apart with the same swizzle.  (Contiguous rows past the tile's last are other rows of x, or past
+  // its end, where the range check, BIG: a clamp, keeps the copy inside.)
+  constexpr int A_REGS = MODE == UP ? A_OPS : 2;
+  using Off = typename std::conditional<BIG && MODE == UP, size_t, uint32_t>::type;
+  int a_tile = -1, a_k = nk, a_rot = 0, a_ops = 0, a_row0 = 0, na_rot = 0, na_ops = 0, na_row0 = 0;
   bool na_ready = false, na_gather = false;
-  Off a_off[A_OPS];
-  int na_row[A_OPS];
+  Off a_off[A_REGS];
+  int na_row[A_REGS];
   auto set_a = [&](const Tile& t) {
     const int valid = t.row_end - t.row0;
     // copies wholly past the expert's last row are not issued; rows past it inside a 32-row block
@@ -301,18 +354,23 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
     na_ops = __builtin_amdgcn_readfirstlane(min(max(n, 0), A_OPS));
     na_rot = t.rot;
     na_gather = MODE == UP && t.expert != E;
+    na_row0 = valid > 0 ? t.row0 : 0;
+    if constexpr (MODE == UP) {
 #pragma unroll
-    for (int j = 0; j < A_OPS; ++j) {
-      const int r = lane_row(A_OPS * wave + j);
-      int src = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
-      if (MODE == UP && !na_gather) src -= a.sh_row0;
-      na_row[j] = src;
+      for (int j = 0; j < A_OPS; ++j) {
+        const int r = lane_row(A_OPS * wave + j);
+        int src = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
+        if (!na_gather) src -= a.sh_row0;
+        na_row[j] = src;
+      }
     }
   };
   auto gather_a = [&]() {
-    if (MODE == UP && na_ready && na_gather) {
+    if constexpr (MODE == UP) {
+      if (na_ready && na_gather) {
 #pragma unroll
-      for (int j = 0; j < A_OPS; ++j) na_row[j] = a.gather[na_row[j]];
+        for (int j = 0; j < A_OPS; ++j) na_row[j] = a.gather[na_row[j]];
+      }
     }
   };
   int b_tile = -1, b_k = nk, b_rot = 0, nb_rot = 0, b_len = 0, nb_len = 0;
@@ -354,10 +412,12 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
         a_k = 0;
         a_rot = 4 * na_rot;
         a_ops = na_ops;
+        a_row0 = na_row0;
 #pragma unroll
-        for (int j = 0; j < A_OPS; ++j) {
-          const int src = min(max(na_row[j], 0), a.x_rows - 1);
-          a_off[j] = static_cast<Off>(src) * static_cast<Off>(K) + static_cast<Off>(lane_chunk(A_OPS * wave + j));
+        for (int j = 0; j < A_REGS; ++j) {
+          const int at = A_OPS * wave + j;
+          const int src = MODE == UP ? min(max(na_row[j], 0), a.x_rows - 1) : na_row0 + lane_row(at);
+          a_off[j] = static_cast<Off>(src) * static_cast<Off>(K) + static_cast<Off>(lane_chunk(at));
         }
       } else {
         a_k = nk - 1;
@@ -392,10 +452,14 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
       BIG ? 0 : static_cast<int>(static_cast<uint32_t>(a.x_rows) * static_cast<uint32_t>(K)), 0x00020000);
   auto copy_a = [&](int j, uint8_t* slot, int k0) {
     uint8_t* to = slot + (A_OPS * wave + j) * 1024;
-    if constexpr (BIG) {
+    if constexpr (BIG && MODE == UP) {
       copy_far(a.x + a_off[j] + k0, to);
+    } else if constexpr (BIG) {
+      const int row = min(a_row0 + lane_row(A_OPS * wave + j), a.x_rows - 1);
+      copy_far(a.x + static_cast<size_t>(row) * K + lane_chunk(A_OPS * wave + j) + k0, to);
     } else {
-      const uint32_t off = j < a_ops ? a_off[j] + static_cast<uint32_t>(k0) : 0x80000000u;
+      const uint32_t at = MODE == UP ? a_off[j] : a_off[j % 2] + static_cast<uint32_t>(16 * (j / 2) * K);
+      const uint32_t off = j < a_ops ? at + static_cast<uint32_t>(k0) : 0x80000000u;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (__attribute__((address_space(3))) void*)to, 16, off, 0, 0,
                                                kCopyPolicy);
     }
@@ -411,9 +475,12 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
         rsrc, (__attribute__((address_space(3))) void*)(slot + (B_OPS * wave + j) * 1024), 16, off, 0, 0, kCopyPolicy);
   };
   // ---- multiply: pair blocks WM i + wm, weight blocks b_row[j] of the tile
-  const int b_row[G8_NJ] = {MODE == UP ? 32 * wn : 64 * wn, MODE == UP ? S::BROWS / 2 + 32 * wn : 64 * wn + 32};
+  // (UP: two blocks of gate rows, then the matching two of up rows)
+  int b_row[G8_NJ];
+#pragma unroll
+  for (int j = 0; j < G8_NJ; ++j)
+    b_row[j] = MODE == UP ? (j / 2) * (S::BROWS / 2) + 64 * wn + 32 * (j % 2) : 128 * wn + 32 * j;
   const int frow = lane & 31, fsel = lane >> 5, fx = (frow / 2) % G8_CHUNKS;
-  f32x16_t acc[MI][G8_NJ];
   // ---- scales: source rows of this lane's row of each pair block, of this tile and of the next;
   // their bytes of the current group; the weights' bytes of all K (UP: gate and up rows)
   int s_row[MI], ns_row[MI];
@@ -427,7 +494,7 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
       if (MODE == UP) src = t.expert == E ? src - a.sh_row0 : a.gather[src];
       ns_row[i] = src;
     }
-    const int block = min(t.n0 + (MODE == UP ? 0 : 64 * wn), N - 1) / F8_BLOCK;
+    const int block = min(t.n0 + (MODE == UP ? 0 : 128 * wn), N - 1) / F8_BLOCK;
     const size_t stride = static_cast<size_t>((N + F8_BLOCK - 1) / F8_BLOCK) * groups;
 #pragma unroll
     for (int j = 0; j < (MODE == UP ? 2 : 1); ++j) {
@@ -459,6 +526,14 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
 #pragma unroll
     for (int j = 0; j < A_OPS; ++j) copy_a(j, a_ring + q * S::A_BYTES, k);
   }
+  // The K loop of one tile with NB active pair blocks (0: this wave only copies), group by group; at its
+  // end s_cur holds the next tile's first group.
+  //
+  // A SIMD has one wave, so the wave itself keeps its matrix core fed: a unit is one pair block times the
+  // four weight blocks of half a slice (four MFMAs, 256 cycles), a slice 2 NB units.  A unit's fragments
+  // are read while an earlier one multiplies, and a slice's last LATE units run after the next step's
+  // barrier, while that slice's first fragments are read.  Units alternate between two fragment
+  // registers; the late ones have their own.
   Tile t = tile_at(0), next_t = t;
   set_scales(t);
   take_scales();
@@ -466,11 +541,46 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
   for (int i = 0; i < MI; ++i) load_scale(i, s_row[i], t.rot);
   wait_copies<0>();       // (not in the order that the steps count on)
   int s = 0;              // steps so far (the rings' slot counter)
-  // The K loop of one tile with NB active pair blocks (0: this wave only copies), group by group;
-  // at its end s_cur holds the next tile's first group.
-  auto k_loop = [&](auto nb_c) {
+  // One tile: K loop and epilogue, an instance per count of active blocks (with the accumulators inside,
+  // which would be copied together from five places otherwise).
+  auto tile = [&](auto nb_c) {
     constexpr int NB = decltype(nb_c)::value;
-    auto step = [&](const uint32_t (&sx)[MI], const uint32_t (&sw)[2]) {
+    f32x16_t acc[NB > 0 ? NB : 1][G8_NJ];
+    constexpr int UNITS = 2 * NB, LATE = NB > 1 ? 2 : 1;
+    i32x8_t af[2 + LATE], bf[2][G8_NJ];
+    uint32_t late_sx[LATE], late_sw[2];      // the late units' scales
+    auto slot_of = [](int u) { return u >= UNITS - LATE ? 2 + u - (UNITS - LATE) : u % 2; };
+    // (fresh: the first products of a tile add to nothing)
+    auto multiply = [&](auto fresh_c, int u, uint32_t sx, const uint32_t (&sw)[2]) {
+      constexpr bool FRESH = decltype(fresh_c)::value;
+      const f32x16_t zero = {};
+      const int kk = u / (NB > 0 ? NB : 1), i = u - kk * NB;
+      // weights as the MFMA's A operand: a lane ends up with 4 consecutive columns of one row
+      if constexpr (WIDE) {
+        const float sws = __uint_as_float((sw[0] & 0xffu) << 23);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bf16x8_t xb =
+              widen8(af[slot_of(u)][2 * q], af[slot_of(u)][2 * q + 1], __uint_as_float((sx & 0xffu) << 23));
+#pragma unroll
+          for (int j = 0; j < G8_NJ; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(bf[kk][j][2 * q], bf[kk][j][2 * q + 1], sws), xb,
+                                                                FRESH && q == 0 ? zero : acc[i][j], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < G8_NJ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+              bf[kk][j], af[slot_of(u)], FRESH ? zero : acc[i][j], 0, 0, 0, static_cast<int>(sw[MODE == UP ? j / 2 : 0]), 0,
+              static_cast<int>(sx));
+      }
+    };
+    auto late_units = [&]() {
+#pragma unroll
+      for (int l = 0; l < LATE; ++l) multiply(std::false_type{}, UNITS - LATE + l, late_sx[l], late_sw);
+    };
+    auto step = [&](auto first_c, const uint32_t (&sx)[MI], const uint32_t (&sw)[2]) {
+      constexpr bool FIRST = decltype(first_c)::value;
       const int ka = a_next(), kb = b_next();
       // slice s has landed (copies land in order; other outstanding accesses only lengthen the
       // wait) and is visible to all waves; the slots that the previous step read are free
@@ -478,52 +588,88 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
       lds_barrier8();
       uint8_t* const An = a_ring + ((s + S::A_SLOTS - 1) % S::A_SLOTS) * S::A_BYTES;
       uint8_t* const Bn = b_ring + ((s + S::B_SLOTS - 1) % S::B_SLOTS) * S::B_BYTES;
-      const uint8_t* const As = a_ring + (s % S::A_SLOTS) * S::A_BYTES;
-      const uint8_t* const Bs = b_ring + (s % S::B_SLOTS) * S::B_BYTES;
-      auto read = [&](const uint8_t* row, int kk) {
-        const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(row + ((4 * kk + fsel) ^ fx) * 16);
-        const i32x4_t hi = *reinterpret_cast<const i32x4_t*>(row + ((4 * kk + 2 + fsel) ^ fx) * 16);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      };
+      if constexpr (NB == 0) {
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        i32x8_t af[MI], bf[G8_NJ];
-        if constexpr (NB > 0) {
+        for (int j = 0; j < A_OPS; ++j) copy_a(j, An, ka);
 #pragma unroll
-          for (int j = 0; j < G8_NJ; ++j) bf[j] = read(Bs + (b_row[j] + frow) * G8_BK, kk);
+        for (int j = 0; j < B_OPS; ++j) copy_b(j, Bn, kb);
+      } else {
+        constexpr int kMfmas = WIDE ? 4 * G8_NJ : G8_NJ;      // of a unit
+        const uint8_t* const As = a_ring + (s % S::A_SLOTS) * S::A_BYTES;
+        const uint8_t* const Bs = b_ring + (s % S::B_SLOTS) * S::B_BYTES;
+        auto read = [&](const uint8_t* row, int kk) {
+          const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(row + ((4 * kk + fsel) ^ fx) * 16);
+          const i32x4_t hi = *reinterpret_cast<const i32x4_t*>(row + ((4 * kk + 2 + fsel) ^ fx) * 16);
+          return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto read_b = [&](int kk, int j) { bf[kk][j] = read(Bs + (b_row[j] + frow) * G8_BK, kk); };
+        auto read_a = [&](int u) {
+          const int kk = u / NB, i = u - kk * NB;
+          af[slot_of(u)] = read(As + (32 * (S::WM * i + wm) + frow) * G8_BK, kk);
+        };
+        // The copies, a few after each unit.
+        constexpr int SPOTS = FIRST ? UNITS - LATE : UNITS, OPS = A_OPS + B_OPS;
+        int done = 0, spot = 0;
+        auto copies = [&](int spots) {
+          spot += spots;
+          const int until = spot >= SPOTS ? OPS : OPS * spot / SPOTS;
 #pragma unroll
-          for (int i = 0; i < NB; ++i) af[i] = read(As + (32 * (S::WM * i + wm) + frow) * G8_BK, kk);
-        }
-        if (kk == 0) {
-#pragma unroll
-          for (int j = 0; j < A_OPS; ++j) copy_a(j, An, ka);
-        } else {
-#pragma unroll
-          for (int j = 0; j < B_OPS; ++j) copy_b(j, Bn, kb);
-        }
-        // weights as the MFMA's A operand: a lane ends up with 4 consecutive columns of one row
-        if constexpr (WIDE) {
-          const float sws = __uint_as_float((sw[0] & 0xffu) << 23);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            bf16x8_t wb[G8_NJ];
-#pragma unroll
-            for (int j = 0; j < G8_NJ; ++j) wb[j] = widen8(bf[j][2 * q], bf[j][2 * q + 1], sws);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-              const bf16x8_t xb = widen8(af[i][2 * q], af[i][2 * q + 1], __uint_as_float((sx[i] & 0xffu) << 23));
-#pragma unroll
-              for (int j = 0; j < G8_NJ; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], xb, acc[i][j], 0, 0, 0);
+          for (int c = 0; c < OPS; ++c)
+            if (c >= done && c < until) {
+              if (c < A_OPS)
+                copy_a(c, An, ka);
+              else
+                copy_b(c - A_OPS, Bn, kb);
+              __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
             }
+          done = until;
+        };
+#pragma unroll
+        for (int j = 0; j < G8_NJ; ++j) read_b(0, j);
+        // (not the late units' yet: their registers hold the previous slice's)
+        constexpr int AHEAD = UNITS - LATE < 2 ? UNITS - LATE : 2;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) read_a(u);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * G8_NJ + 2 * AHEAD, 0);
+        if constexpr (!FIRST) {
+#pragma unroll
+          for (int l = 0; l < LATE; ++l) {
+            multiply(std::false_type{}, UNITS - LATE + l, late_sx[l], late_sw);
+            __builtin_amdgcn_sched_group_barrier(0x008, kMfmas, 0);
+            copies(1);
           }
-        } else
+        }
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
+        for (int u = 0; u < UNITS - LATE; ++u) {
+          // what is read during this unit: its share of the second half's weights, a later unit's rows
+          int reads = 0;
+          if (u < NB) {
 #pragma unroll
-          for (int j = 0; j < G8_NJ; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                bf[j], af[i], acc[i][j], 0, 0, 0, static_cast<int>(sw[MODE == UP ? j : 0]), 0, static_cast<int>(sx[i]));
+            for (int j = 0; j < G8_NJ; ++j)
+              if (j >= G8_NJ * u / NB && j < G8_NJ * (u + 1) / NB) {
+                read_b(1, j);
+                reads += 2;
+              }
+          }
+          if (FIRST && u < NB)
+            multiply(std::true_type{}, u, sx[u % (NB > 0 ? NB : 1)], sw);
+          else
+            multiply(std::false_type{}, u, sx[u % (NB > 0 ? NB : 1)], sw);
+          if (u + AHEAD < UNITS) {
+            read_a(u + AHEAD);
+            reads += 2;
+          }
+          if (reads == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          if (reads == 4) __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+          if (reads == 6) __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+          if (reads == 10) __builtin_amdgcn_sched_group_barrier(0x100, 10, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, kMfmas, 0);
+          copies(1);
+        }
+#pragma unroll
+        for (int l = 0; l < LATE; ++l) late_sx[l] = sx[(UNITS - LATE + l) % NB];
+        late_sw[0] = sw[0];
+        late_sw[1] = sw[1];
       }
     };
     int g = t.rot;
@@ -539,16 +685,120 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
       g = last ? next_t.rot : (g + 1 < groups ? g + 1 : 0);
 #pragma unroll
       for (int i = 0; i < MI; ++i) load_scale(i, last ? ns_row[i] : s_row[i], g);
-      for (int q = 0; q < len; ++q, ++s) {
-        step(sx, sw);
+      int q = 0;
+      auto shift = [&]() {
 #pragma unroll
         for (int i = 0; i < MI; ++i) sx[i] >>= 8;
 #pragma unroll
         for (int j = 0; j < 2; ++j) sw[j] >>= 8;
+        ++q;
+        ++s;
+      };
+      if (done == 0) {
+        step(std::true_type{}, sx, sw);
+        shift();
+      }
+      while (q < len) {
+        step(std::false_type{}, sx, sw);
+        shift();
       }
       done += len;
     }
+    if constexpr (NB > 0) late_units();
     take_scales();
+    // every wave has read the tile's last slices: the weight slot takes the epilogue's scratch (the
+    // next tile's first step refills it only after its own barrier)
+    lds_barrier8();
+    const uint32_t scratch = static_cast<uint32_t>(
+        reinterpret_cast<uintptr_t>(b_ring + ((s + S::B_SLOTS - 1) % S::B_SLOTS) * S::B_BYTES));
+    if constexpr (MODE == UP) {
+      // the activation and its rows' maxima over this wave's 32 columns; then the codes, with the
+      // maximum of the four waves that share the rows
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        __builtin_amdgcn_sched_barrier(0);      // (one block's registers at a time)
+        {
+          uint32_t m = 0, lo, hi;
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float v = silu_mul(acc[i][jj][r], acc[i][jj + 2][r]);
+              acc[i][jj][r] = v;
+              const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+              m = max(m, b < 0x7f800000u ? b : 0u);
+            }
+          rows_swap32(m, lo, hi);
+          asm volatile("ds_write_b32 %0, %1" ::"v"(scratch + 8u * (32 * (S::WM * i + wm) + frow) + 4u * wn),
+                       "v"(max(lo, hi)) : "memory");
+        }
+      }
+      lds_barrier8();
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        __builtin_amdgcn_sched_barrier(0);      // (one block's registers at a time)
+        {
+          const int in_tile = 32 * (S::WM * i + wm) + frow, row = t.row0 + in_tile;
+          u32x2_t both;
+          asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(both) : "v"(scratch + 8u * in_tile) : "memory");
+          const uint32_t byte = f8_scale_byte(max(both[0], both[1]));
+          const float inv = f8_inverse(byte);
+          const int kb = t.n0 / F8_BLOCK;
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) {
+            uint32_t v[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const f32x16_t& c = acc[i][jj];
+              v[g] = f8_pack4(c[4 * g] * inv, c[4 * g + 1] * inv, c[4 * g + 2] * inv, c[4 * g + 3] * inv);
+#pragma unroll
+              for (int h = 0; h < 4; ++h)       // infinities and NaN: the one NaN code
+                if ((__float_as_uint(c[4 * g + h]) & 0x7fffffffu) >= 0x7f800000u)
+                  v[g] = (v[g] & ~(0xffu << (8 * h))) | (0x7fu << (8 * h));
+            }
+            // a lane holds columns 8 g + 4 fsel ..; with the wave's halves swapped the lower one holds
+            // columns 0-15 of each row, the upper one 16-31
+            const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+            const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+            if (row < t.row_end)
+              *reinterpret_cast<u32x4_t*>(static_cast<uint8_t*>(a.out) + static_cast<size_t>(row) * N + t.n0 + 64 * wn +
+                                          32 * jj + 16 * fsel) = u32x4_t{p[0], p[1], q[0], q[1]};
+          }
+          if (row < t.row_end && wn == 0 && fsel == 0)
+            a.out_scale[(static_cast<size_t>(kb >> 2) * a.act_rows + row) * 4 + (kb & 3)] = static_cast<uint8_t>(byte);
+        }
+      }
+    } else {
+      OUT* const out = static_cast<OUT*>(a.out);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        __builtin_amdgcn_sched_barrier(0);      // (one block's registers at a time)
+        {
+          const int rb = t.row0 + 32 * (S::WM * i + wm);
+          const uint32_t stage = scratch + wave * G8_STAGE;
+#pragma unroll
+          for (int j = 0; j < G8_NJ; j += sizeof(OUT) == 4 ? 1 : 2) {
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (sizeof(OUT) == 4) {
+              const f32x16_t& c = acc[i][j];
+#pragma unroll
+              for (int g = 0; g < 4; ++g)
+                lds_write128(stage_at(stage, frow, 2 * g + fsel), c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]);
+            } else {
+#pragma unroll
+              for (int jj = 0; jj < 2; ++jj) {
+                const f32x16_t& c = acc[i][j + jj];
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                  lds_write64(stage_at(stage, frow, 4 * jj + g) + 8 * fsel, pack_bf16x2(c[4 * g], c[4 * g + 1]),
+                              pack_bf16x2(c[4 * g + 2], c[4 * g + 3]));
+              }
+            }
+            store_staged<OUT, MODE == PLAIN>(rb, t.n0 + 128 * wn + 32 * j, t.row_end, N, out, stage);
+          }
+        }
+      }
+    }
   };
   for (int tile_i = 0; tile_i < n_my; ++tile_i) {
     const bool more = tile_i + 1 < n_my;
@@ -567,97 +817,18 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
     // pair blocks of this wave that hold pairs: blocks wm, wm + WM, .. of the tile
     const int blocks = (t.row_end - t.row0 + 31) >> 5;
     const int nb = __builtin_amdgcn_readfirstlane(min(max(blocks - wm + S::WM - 1, 0) / S::WM, MI));
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int j = 0; j < G8_NJ; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    switch (nb) {      // one instance of the K loop per count of active blocks
+    switch (nb) {
       case 4:
-        if constexpr (MI >= 4) k_loop(std::integral_constant<int, 4>{});
+        if constexpr (MI >= 4) tile(std::integral_constant<int, 4>{});
         break;
       case 3:
-        if constexpr (MI >= 3) k_loop(std::integral_constant<int, 3>{});
+        if constexpr (MI >= 3) tile(std::integral_constant<int, 3>{});
         break;
       case 2:
-        if constexpr (MI >= 2) k_loop(std::integral_constant<int, 2>{});
+        if constexpr (MI >= 2) tile(std::integral_constant<int, 2>{});
         break;
-      case 1: k_loop(std::integral_constant<int, 1>{}); break;
-      default: k_loop(std::integral_constant<int, 0>{}); break;
-    }
-    // every wave has read the tile's last slices: the weight slot takes the epilogue's scratch (the
-    // next tile's first step refills it only after its own barrier)
-    lds_barrier8();
-    const uint32_t scratch = static_cast<uint32_t>(
-        reinterpret_cast<uintptr_t>(b_ring + ((s + S::B_SLOTS - 1) % S::B_SLOTS) * S::B_BYTES));
-    if constexpr (MODE == UP) {
-      // the activation and its rows' maxima over this wave's 32 columns; then the codes, with the
-      // maximum of the four waves that share the rows
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        if (i < nb) {
-          uint32_t m = 0, lo, hi;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float v = silu_mul(acc[i][0][r], acc[i][1][r]);
-            acc[i][0][r] = v;
-            const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-            m = max(m, b < 0x7f800000u ? b : 0u);
-          }
-          rows_swap32(m, lo, hi);
-          asm volatile("ds_write_b32 %0, %1" ::"v"(scratch + 16u * (32 * (S::WM * i + wm) + frow) + 4u * wn),
-                       "v"(max(lo, hi)) : "memory");
-        }
-      }
-      lds_barrier8();
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        if (i < nb) {
-          const int in_tile = 32 * (S::WM * i + wm) + frow, row = t.row0 + in_tile;
-          u32x4_t m4;
-          asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(m4) : "v"(scratch + 16u * in_tile) : "memory");
-          const uint32_t byte = f8_scale_byte(max(max(m4[0], m4[1]), max(m4[2], m4[3])));
-          const float inv = f8_inverse(byte);
-          uint32_t v[4];
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const f32x16_t& c = acc[i][0];
-            v[g] = f8_pack4(c[4 * g] * inv, c[4 * g + 1] * inv, c[4 * g + 2] * inv, c[4 * g + 3] * inv);
-#pragma unroll
-            for (int h = 0; h < 4; ++h)       // infinities and NaN: the one NaN code
-              if ((__float_as_uint(c[4 * g + h]) & 0x7fffffffu) >= 0x7f800000u)
-                v[g] = (v[g] & ~(0xffu << (8 * h))) | (0x7fu << (8 * h));
-          }
-          // a lane holds columns 8 g + 4 fsel ..; with the wave's halves swapped the lower one holds
-          // columns 0-15 of each row, the upper one 16-31
-          const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
-          const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-          if (row < t.row_end) {
-            uint8_t* to = static_cast<uint8_t*>(a.out) + static_cast<size_t>(row) * N + t.n0 + 32 * wn + 16 * fsel;
-            *reinterpret_cast<u32x4_t*>(to) = u32x4_t{p[0], p[1], q[0], q[1]};
-            const int kb = t.n0 / F8_BLOCK;
-            if (wn == 0 && fsel == 0)
-              a.out_scale[(static_cast<size_t>(kb >> 2) * a.act_rows + row) * 4 + (kb & 3)] = static_cast<uint8_t>(byte);
-          }
-        }
-      }
-    } else {
-      OUT* const out = static_cast<OUT*>(a.out);
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        if (i < nb) {
-          const int rb = t.row0 + 32 * (S::WM * i + wm);
-#pragma unroll
-          for (int j = 0; j < G8_NJ; ++j) {
-            const int cb = t.n0 + 64 * wn + 32 * j;
-            if constexpr (MODE == PLAIN)
-              store_any(acc[i][j], rb, cb, t.row_end, N, out);
-            else
-              store_bf16(acc[i][j], rb, cb, t.row_end, N, out, scratch + wave * G8_STAGE);
-          }
-        }
-      }
+      case 1: tile(std::integral_constant<int, 1>{}); break;
+      default: tile(std::integral_constant<int, 0>{}); break;
     }
     t = next_t;
   }
@@ -666,9 +837,9 @@ __global__ __launch_bounds__(S::THREADS) void fp8_gemm_kernel(Args8 a) {
 
 // The tile shapes (pair rows x weight rows).  The activation's blocks of 128 columns need 256
 // weight rows a tile (128 of gate, 128 of up).
-using Tall = Shape8<4, 2, 4, 2, 3>;       // 256 x 256, 160 KB of LDS, one workgroup per CU
-using Half = Shape8<2, 2, 4, 3, 3>;       // 128 x 256, 144 KB
-using Quarter = Shape8<1, 2, 4, 3, 4>;    // 64 x 256, 152 KB
+using Tall = Shape8<4, 2, 3>;       // 256 x 256, 160 KB of LDS, one workgroup per CU
+using Half = Shape8<2, 3, 3>;       // 128 x 256, 144 KB
+using Quarter = Shape8<1, 3, 4>;    // 64 x 256, 152 KB
 
 template <Mode MODE, class S, bool BIG, class OUT>
 int launch_as(const Args8& a, hipStream_t s) {
