@@ -95,6 +95,14 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)) * u;
 }
 
+// The lane number, as a value that is computed where it is used: what depends on it is not moved out of the
+// loops around, where it would hold registers over a whole tile.
+__device__ __forceinline__ int lane_here() {
+  int l = threadIdx.x & 63;
+  asm volatile("" : "+v"(l));
+  return l;
+}
+
 // ---- epilogue stores of a plain tile ---------------------------------------------------------
 // A wave has 32 rows x 128 columns of a pair block as four accumulators of 32 columns: lane l, register r
 // holds row l % 32 and column 8 (r/4) + 4 (l/32) + r%4.  Rows go through the wave's 4 KB of scratch in
@@ -120,7 +128,7 @@ template <class OUT, bool ANY_N>
 __device__ __forceinline__ void store_staged(int row_base, int col_base, int row_end, int N, OUT* __restrict__ out,
                                              uint32_t stage) {
   constexpr int COLS = 128 / sizeof(OUT), VEC = 16 / sizeof(OUT);
-  const int lane = threadIdx.x & 63;
+  const int lane = lane_here();
   if (!ANY_N || N % VEC == 0) {      // whole vectors: 8 lanes a row
     u32x4_t v[4];
     uint32_t at[4];
@@ -335,8 +343,8 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   // current tile and slice and holds the next tile's setup ready: a tile's K loop takes it
   // across one tile boundary at most (unless short_k, when setups are made at the boundary).
   const bool short_k = nk < S::B_SLOTS;
-  auto lane_row = [&](int q) { return q * G8_OP_ROWS + lane / G8_CHUNKS; };
-  auto lane_chunk = [&](int q) { return ((lane % G8_CHUNKS) ^ ((lane_row(q) / 2) % G8_CHUNKS)) * 16; };
+  auto lane_row = [](int l, int q) { return q * G8_OP_ROWS + l / G8_CHUNKS; };
+  auto lane_chunk = [&](int l, int q) { return ((l % G8_CHUNKS) ^ ((lane_row(l, q) / 2) % G8_CHUNKS)) * 16; };
   // Gathered rows (UP) have an offset a copy; contiguous ones a first row, copies j and j + 2 being 16 rows
   // apart with the same swizzle.  (Contiguous rows past the tile's last are other rows of x, or past
   // its end, where the range check, BIG: a clamp, keeps the copy inside.)
@@ -345,7 +353,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   int a_tile = -1, a_k = nk, a_rot = 0, a_ops = 0, a_row0 = 0, na_rot = 0, na_ops = 0, na_row0 = 0;
   bool na_ready = false, na_gather = false;
   Off a_off[A_REGS];
-  int na_row[A_REGS];
+  int na_row = 0;      // UP: lane l has the source row of the wave's row l of the next tile
   auto set_a = [&](const Tile& t) {
     const int valid = t.row_end - t.row0;
     // copies wholly past the expert's last row are not issued; rows past it inside a 32-row block
@@ -356,21 +364,14 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
     na_gather = MODE == UP && t.expert != E;
     na_row0 = valid > 0 ? t.row0 : 0;
     if constexpr (MODE == UP) {
-#pragma unroll
-      for (int j = 0; j < A_OPS; ++j) {
-        const int r = lane_row(A_OPS * wave + j);
-        int src = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
-        if (!na_gather) src -= a.sh_row0;
-        na_row[j] = src;
-      }
+      const int r = G8_OP_ROWS * A_OPS * wave + lane_here() % (G8_OP_ROWS * A_OPS);
+      na_row = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
+      if (!na_gather) na_row -= a.sh_row0;
     }
   };
   auto gather_a = [&]() {
     if constexpr (MODE == UP) {
-      if (na_ready && na_gather) {
-#pragma unroll
-        for (int j = 0; j < A_OPS; ++j) na_row[j] = a.gather[na_row[j]];
-      }
+      if (na_ready && na_gather) na_row = a.gather[na_row];
     }
   };
   int b_tile = -1, b_k = nk, b_rot = 0, nb_rot = 0, b_len = 0, nb_len = 0;
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   uint32_t b_lo = 0, b_hi = 0, nb_lo = 0, nb_hi = 0;
   uint32_t b_off[2];       // copies j and j + 2 are 16 rows apart and share the swizzle
 #pragma unroll
-  for (int j = 0; j < 2; ++j) b_off[j] = static_cast<uint32_t>(lane_row(j) * K + lane_chunk(B_OPS * wave + j));
+  for (int j = 0; j < 2; ++j) b_off[j] = static_cast<uint32_t>(lane_row(lane, j) * K + lane_chunk(lane, B_OPS * wave + j));
   auto set_b = [&](const Tile& t) {
     nb_rot = t.rot;
     constexpr int W = S::B_WROWS, HALF = S::WAVES / 2;
@@ -413,11 +414,12 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
         a_rot = 4 * na_rot;
         a_ops = na_ops;
         a_row0 = na_row0;
+        const int l = lane_here();
 #pragma unroll
         for (int j = 0; j < A_REGS; ++j) {
           const int at = A_OPS * wave + j;
-          const int src = MODE == UP ? min(max(na_row[j], 0), a.x_rows - 1) : na_row0 + lane_row(at);
-          a_off[j] = static_cast<Off>(src) * static_cast<Off>(K) + static_cast<Off>(lane_chunk(at));
+          const int src = MODE == UP ? min(max(__shfl(na_row, lane_row(l, j)), 0), a.x_rows - 1) : na_row0 + lane_row(l, at);
+          a_off[j] = static_cast<Off>(src) * static_cast<Off>(K) + static_cast<Off>(lane_chunk(l, at));
         }
       } else {
         a_k = nk - 1;
@@ -455,8 +457,8 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
     if constexpr (BIG && MODE == UP) {
       copy_far(a.x + a_off[j] + k0, to);
     } else if constexpr (BIG) {
-      const int row = min(a_row0 + lane_row(A_OPS * wave + j), a.x_rows - 1);
-      copy_far(a.x + static_cast<size_t>(row) * K + lane_chunk(A_OPS * wave + j) + k0, to);
+      const int l = lane_here(), row = min(a_row0 + lane_row(l, A_OPS * wave + j), a.x_rows - 1);
+      copy_far(a.x + static_cast<size_t>(row) * K + lane_chunk(l, A_OPS * wave + j) + k0, to);
     } else {
       const uint32_t at = MODE == UP ? a_off[j] : a_off[j % 2] + static_cast<uint32_t>(16 * (j / 2) * K);
       const uint32_t off = j < a_ops ? at + static_cast<uint32_t>(k0) : 0x80000000u;
@@ -480,35 +482,32 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
 #pragma unroll
   for (int j = 0; j < G8_NJ; ++j)
     b_row[j] = MODE == UP ? (j / 2) * (S::BROWS / 2) + 64 * wn + 32 * (j % 2) : 128 * wn + 32 * j;
-  const int frow = lane & 31, fsel = lane >> 5, fx = (frow / 2) % G8_CHUNKS;
   // ---- scales: source rows of this lane's row of each pair block, of this tile and of the next;
   // their bytes of the current group; the weights' bytes of all K (UP: gate and up rows)
-  int s_row[MI], ns_row[MI];
-  uint32_t s_cur[MI], w_cur[2] = {0, 0}, w_next[2] = {0, 0};
+  constexpr int SR = (MI + 1) / 2;      // lane l has row l % 32 of pair block 2 q + l / 32
+  int s_row[SR], ns_row[SR];
+  uint32_t s_cur[SR], w_cur[2] = {0, 0}, w_next[2] = {0, 0};
   auto set_scales = [&](const Tile& t) {
-    const int valid = t.row_end - t.row0;
+    const int valid = t.row_end - t.row0, l = lane_here();
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int r = 32 * (S::WM * i + wm) + frow;
+    for (int q = 0; q < SR; ++q) {
+      const int r = 32 * (S::WM * (2 * q + l / 32) + wm) + l % 32;
       int src = valid > 0 ? t.row0 + (r < valid ? r : 0) : 0;
       if (MODE == UP) src = t.expert == E ? src - a.sh_row0 : a.gather[src];
-      ns_row[i] = src;
+      ns_row[q] = min(max(src, 0), a.x_rows - 1);
     }
     const int block = min(t.n0 + (MODE == UP ? 0 : 128 * wn), N - 1) / F8_BLOCK;
     const size_t stride = static_cast<size_t>((N + F8_BLOCK - 1) / F8_BLOCK) * groups;
 #pragma unroll
     for (int j = 0; j < (MODE == UP ? 2 : 1); ++j) {
       const uint32_t* base = t.expert == E ? (j ? a.ss1 : a.ss0) : (j ? a.s1 : a.s0) + t.expert * stride;
-      w_next[j] = lane < groups ? base[static_cast<size_t>(block) * groups + lane] : 0u;
+      w_next[j] = l < groups ? base[static_cast<size_t>(block) * groups + l] : 0u;
     }
   };
-  auto load_scale = [&](int i, int row, int group) {
-    row = min(max(row, 0), a.x_rows - 1);
-    s_cur[i] = a.x_scale[static_cast<size_t>(group) * a.x_rows + row];
-  };
+  auto load_scale = [&](int q, int row, int group) { s_cur[q] = a.x_scale[static_cast<size_t>(group) * a.x_rows + row]; };
   auto take_scales = [&]() {      // the next tile's become the current tile's
 #pragma unroll
-    for (int i = 0; i < MI; ++i) s_row[i] = ns_row[i];
+    for (int q = 0; q < SR; ++q) s_row[q] = ns_row[q];
     w_cur[0] = w_next[0];
     w_cur[1] = w_next[1];
   };
@@ -538,13 +537,14 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   set_scales(t);
   take_scales();
 #pragma unroll
-  for (int i = 0; i < MI; ++i) load_scale(i, s_row[i], t.rot);
+  for (int q = 0; q < SR; ++q) load_scale(q, s_row[q], t.rot);
   wait_copies<0>();       // (not in the order that the steps count on)
   int s = 0;              // steps so far (the rings' slot counter)
   // One tile: K loop and epilogue, an instance per count of active blocks (with the accumulators inside,
   // which would be copied together from five places otherwise).
   auto tile = [&](auto nb_c) {
     constexpr int NB = decltype(nb_c)::value;
+    const int l = lane_here(), frow = l & 31, fsel = l >> 5, fx = (frow / 2) % G8_CHUNKS;
     f32x16_t acc[NB > 0 ? NB : 1][G8_NJ];
     constexpr int UNITS = 2 * NB, LATE = NB > 1 ? 2 : 1;
     i32x8_t af[2 + LATE], bf[2][G8_NJ];
@@ -678,13 +678,18 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
       const bool last = done + len >= nk;
       uint32_t sx[MI], sw[2];
 #pragma unroll
-      for (int i = 0; i < MI; ++i) sx[i] = s_cur[i];
+      for (int q = 0; q < SR; ++q) {
+        uint32_t lower, upper;      // both halves' rows, in all lanes
+        rows_swap32(s_cur[q], lower, upper);
+        sx[2 * q] = lower;
+        if (2 * q + 1 < MI) sx[2 * q + 1] = upper;
+      }
 #pragma unroll
       for (int j = 0; j < 2; ++j) sw[j] = __builtin_amdgcn_readlane(static_cast<int>(w_cur[j]), g);
       if (done == 0 && !short_k) gather_a();
       g = last ? next_t.rot : (g + 1 < groups ? g + 1 : 0);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) load_scale(i, last ? ns_row[i] : s_row[i], g);
+      for (int q = 0; q < SR; ++q) load_scale(q, last ? ns_row[q] : s_row[q], g);
       int q = 0;
       auto shift = [&]() {
 #pragma unroll
@@ -711,61 +716,78 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
     lds_barrier8();
     const uint32_t scratch = static_cast<uint32_t>(
         reinterpret_cast<uintptr_t>(b_ring + ((s + S::B_SLOTS - 1) % S::B_SLOTS) * S::B_BYTES));
+    const int el = lane_here(), erow = el & 31, esel = el >> 5;
     if constexpr (MODE == UP) {
-      // the activation and its rows' maxima over this wave's 32 columns; then the codes, with the
-      // maximum of the four waves that share the rows
+      // A pair block at a time: the activation and its rows' maxima over this wave's 64 columns, then the
+      // codes, with the maximum of the two waves that share the rows.  All waves pass MI barriers, whatever
+      // their blocks.
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
+      for (int i = 0; i < MI; ++i) {
         __builtin_amdgcn_sched_barrier(0);      // (one block's registers at a time)
-        {
-          uint32_t m = 0, lo, hi;
+        if constexpr (NB > 0) {
+          float v[2][16];
+          uint32_t lo = 0, hi = 0;
+          const int in_tile = 32 * (S::WM * i + wm) + erow, row = t.row0 + in_tile;
+          bool odd = false;      // infinities or NaN in the block
+          if (i < NB) {
+            float m = 0.0f, bad = 0.0f;
 #pragma unroll
-          for (int jj = 0; jj < 2; ++jj)
+            for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float v = silu_mul(acc[i][jj][r], acc[i][jj + 2][r]);
-              acc[i][jj][r] = v;
-              const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-              m = max(m, b < 0x7f800000u ? b : 0u);
+              for (int r = 0; r < 16; ++r) {
+                v[jj][r] = silu_mul(acc[i < NB ? i : 0][jj][r], acc[i < NB ? i : 0][jj + 2][r]);
+                m = fmaxf(m, fabsf(v[jj][r]));
+                bad = fmaf(v[jj][r], 0.0f, bad);
+              }
+            odd = __any(bad != 0.0f);      // (NaN compares unequal)
+            uint32_t mb = __float_as_uint(m);
+            if (odd) {                     // the maximum of the finite values
+              mb = 0;
+#pragma unroll
+              for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  const uint32_t b = __float_as_uint(v[jj][r]) & 0x7fffffffu;
+                  mb = max(mb, b < 0x7f800000u ? b : 0u);
+                }
             }
-          rows_swap32(m, lo, hi);
-          asm volatile("ds_write_b32 %0, %1" ::"v"(scratch + 8u * (32 * (S::WM * i + wm) + frow) + 4u * wn),
-                       "v"(max(lo, hi)) : "memory");
-        }
-      }
-      lds_barrier8();
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        __builtin_amdgcn_sched_barrier(0);      // (one block's registers at a time)
-        {
-          const int in_tile = 32 * (S::WM * i + wm) + frow, row = t.row0 + in_tile;
-          u32x2_t both;
-          asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(both) : "v"(scratch + 8u * in_tile) : "memory");
-          const uint32_t byte = f8_scale_byte(max(both[0], both[1]));
-          const float inv = f8_inverse(byte);
-          const int kb = t.n0 / F8_BLOCK;
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            uint32_t v[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const f32x16_t& c = acc[i][jj];
-              v[g] = f8_pack4(c[4 * g] * inv, c[4 * g + 1] * inv, c[4 * g + 2] * inv, c[4 * g + 3] * inv);
-#pragma unroll
-              for (int h = 0; h < 4; ++h)       // infinities and NaN: the one NaN code
-                if ((__float_as_uint(c[4 * g + h]) & 0x7fffffffu) >= 0x7f800000u)
-                  v[g] = (v[g] & ~(0xffu << (8 * h))) | (0x7fu << (8 * h));
-            }
-            // a lane holds columns 8 g + 4 fsel ..; with the wave's halves swapped the lower one holds
-            // columns 0-15 of each row, the upper one 16-31
-            const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
-            const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-            if (row < t.row_end)
-              *reinterpret_cast<u32x4_t*>(static_cast<uint8_t*>(a.out) + static_cast<size_t>(row) * N + t.n0 + 64 * wn +
-                                          32 * jj + 16 * fsel) = u32x4_t{p[0], p[1], q[0], q[1]};
+            rows_swap32(mb, lo, hi);
+            asm volatile("ds_write_b32 %0, %1" ::"v"(scratch + 8u * in_tile + 4u * wn), "v"(max(lo, hi)) : "memory");
           }
-          if (row < t.row_end && wn == 0 && fsel == 0)
-            a.out_scale[(static_cast<size_t>(kb >> 2) * a.act_rows + row) * 4 + (kb & 3)] = static_cast<uint8_t>(byte);
+          lds_barrier8();
+          if (i < NB) {
+            u32x2_t both;
+            asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(both) : "v"(scratch + 8u * in_tile) : "memory");
+            const uint32_t byte = f8_scale_byte(max(both[0], both[1]));
+            const float inv = f8_inverse(byte);
+            const int kb = t.n0 / F8_BLOCK;
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+              uint32_t c[4];
+#pragma unroll
+              for (int g = 0; g < 4; ++g)
+                c[g] = f8_pack4(v[jj][4 * g] * inv, v[jj][4 * g + 1] * inv, v[jj][4 * g + 2] * inv, v[jj][4 * g + 3] * inv);
+              if (odd) {      // infinities and NaN: the one NaN code
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                  for (int h = 0; h < 4; ++h)
+                    if ((__float_as_uint(v[jj][4 * g + h]) & 0x7fffffffu) >= 0x7f800000u)
+                      c[g] = (c[g] & ~(0xffu << (8 * h))) | (0x7fu << (8 * h));
+              }
+              // a lane holds columns 8 g + 4 esel ..; with the wave's halves swapped the lower one holds
+              // columns 0-15 of each row, the upper one 16-31
+              const auto p = __builtin_amdgcn_permlane32_swap(c[0], c[2], false, false);
+              const auto q = __builtin_amdgcn_permlane32_swap(c[1], c[3], false, false);
+              if (row < t.row_end)
+                *reinterpret_cast<u32x4_t*>(static_cast<uint8_t*>(a.out) + static_cast<size_t>(row) * N + t.n0 + 64 * wn +
+                                            32 * jj + 16 * esel) = u32x4_t{p[0], p[1], q[0], q[1]};
+            }
+            if (row < t.row_end && wn == 0 && esel == 0)
+              a.out_scale[(static_cast<size_t>(kb >> 2) * a.act_rows + row) * 4 + (kb & 3)] = static_cast<uint8_t>(byte);
+          }
+        } else {
+          lds_barrier8();
         }
       }
     } else {
@@ -783,14 +805,14 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
               const f32x16_t& c = acc[i][j];
 #pragma unroll
               for (int g = 0; g < 4; ++g)
-                lds_write128(stage_at(stage, frow, 2 * g + fsel), c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]);
+                lds_write128(stage_at(stage, erow, 2 * g + esel), c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]);
             } else {
 #pragma unroll
               for (int jj = 0; jj < 2; ++jj) {
                 const f32x16_t& c = acc[i][j + jj];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                  lds_write64(stage_at(stage, frow, 4 * jj + g) + 8 * fsel, pack_bf16x2(c[4 * g], c[4 * g + 1]),
+                  lds_write64(stage_at(stage, erow, 4 * jj + g) + 8 * esel, pack_bf16x2(c[4 * g], c[4 * g + 1]),
                               pack_bf16x2(c[4 * g + 2], c[4 * g + 3]));
               }
             }
