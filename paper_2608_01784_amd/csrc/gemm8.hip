@@ -123,84 +123,48 @@ __device__ __forceinline__ uint32_t stage_at(uint32_t stage, int row, int chunk)
 }
 
 // The staged 32 rows x (128 / sizeof(OUT)) columns to `out`: rows row_base .. below row_end, columns
-// col_base .. below N.
+// col_base .. below N.  8 lanes a row, 16 bytes each, at any address that the elements allow (rows of
+// an odd N start anywhere; global stores need no alignment beyond that).
 template <class OUT, bool ANY_N>
 __device__ __forceinline__ void store_staged(int row_base, int col_base, int row_end, int N, OUT* __restrict__ out,
                                              uint32_t stage) {
-  constexpr int COLS = 128 / sizeof(OUT), VEC = 16 / sizeof(OUT);
+  constexpr int VEC = 16 / sizeof(OUT), COLS = 128 / sizeof(OUT);
   const int lane = lane_here();
-  if (!ANY_N || N % VEC == 0) {      // whole vectors: 8 lanes a row
-    u32x4_t v[4];
-    uint32_t at[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) at[q] = stage_at(stage, (lane >> 3) + 8 * q, lane & 7);
-    asm volatile(
-        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
-        : "memory");
-    const int col = col_base + VEC * (lane & 7);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int row = row_base + (lane >> 3) + 8 * q;
-      if (row < row_end && col < N) *reinterpret_cast<u32x4_t*>(out + static_cast<size_t>(row) * N + col) = v[q];
+  if (ANY_N && col_base + COLS > N && N % VEC != 0) {      // the rows' end inside a vector: an element a lane
+#pragma unroll 1
+    for (int q = 0; q < 32 * COLS / 64; ++q) {
+      const int r = (64 / COLS) * q + lane / COLS, c = lane % COLS;
+      const uint32_t at = stage_at(stage, r, c / VEC) + sizeof(OUT) * (c % VEC);
+      uint32_t v;
+      if constexpr (sizeof(OUT) == 4)
+        asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
+      else
+        asm volatile("ds_read_u16 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
+      if (row_base + r < row_end && col_base + c < N) {
+        OUT* const to = out + static_cast<size_t>(row_base + r) * N + col_base + c;
+        if constexpr (sizeof(OUT) == 4)
+          *to = __uint_as_float(v);
+        else
+          *to = static_cast<OUT>(v);
+      }
     }
     return;
   }
-  if constexpr (sizeof(OUT) == 4) {      // dwords: 32 lanes a row
-#pragma unroll 1
-    for (int q = 0; q < 16; q += 4) {
-      uint32_t v[4], at[4];
+  u32x4_t v[4];
+  uint32_t at[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) at[e] = stage_at(stage, (lane >> 5) + 2 * (q + e), (lane & 31) / 4) + 4 * (lane & 3);
-      asm volatile(
-          "ds_read_b32 %0, %4\n\tds_read_b32 %1, %5\n\tds_read_b32 %2, %6\n\tds_read_b32 %3, %7\n\t"
-          "s_waitcnt lgkmcnt(0)"
-          : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
-          : "memory");
+  for (int q = 0; q < 4; ++q) at[q] = stage_at(stage, (lane >> 3) + 8 * q, lane & 7);
+  asm volatile(
+      "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+      : "memory");
+  const int col = col_base + VEC * (lane & 7);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = row_base + (lane >> 5) + 2 * (q + e), col = col_base + (lane & 31);
-        if (row < row_end && col < N) out[static_cast<size_t>(row) * N + col] = __uint_as_float(v[e]);
-      }
-    }
-  } else {
-    // Any N: 32 lanes a row, two columns each as a dword where its address allows: in a row that starts at
-    // an odd element the pairs are columns 1-2, 3-4, .., and lane 31 has the first and the last column.
-#pragma unroll 1
-    for (int q = 0; q < 16; q += 2) {
-      uint32_t v[4], at[4];
-      int first[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = (lane >> 5) + 2 * (q + e), l = lane & 31;
-        const bool odd = ((static_cast<size_t>(row_base + r) * N + col_base) & 1) != 0;
-        first[e] = 2 * l + (odd ? 1 : 0);
-        const int c0 = first[e], c1 = (c0 + 1) % COLS;      // (odd, l = 31: columns 63 and 0)
-        at[2 * e] = stage_at(stage, r, c0 / 8) + 2 * (c0 % 8);
-        at[2 * e + 1] = stage_at(stage, r, c1 / 8) + 2 * (c1 % 8);
-      }
-      asm volatile(
-          "ds_read_u16 %0, %4\n\tds_read_u16 %1, %5\n\tds_read_u16 %2, %6\n\tds_read_u16 %3, %7\n\t"
-          "s_waitcnt lgkmcnt(0)"
-          : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
-          : "memory");
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int row = row_base + (lane >> 5) + 2 * (q + e), c0 = col_base + first[e];
-        if (row >= row_end) continue;
-        OUT* const to = out + static_cast<size_t>(row) * N;
-        if (first[e] + 1 < COLS && c0 + 1 < N) {
-          *reinterpret_cast<uint32_t*>(to + c0) = v[2 * e] | (v[2 * e + 1] << 16);
-        } else {
-          if (c0 < N) to[c0] = static_cast<OUT>(v[2 * e]);
-          if (first[e] + 1 >= COLS && col_base < N) to[col_base] = static_cast<OUT>(v[2 * e + 1]);
-        }
-      }
-    }
+  for (int q = 0; q < 4; ++q) {
+    const int row = row_base + (lane >> 3) + 8 * q;
+    if (row < row_end && col < N) __builtin_memcpy(out + static_cast<size_t>(row) * N + col, &v[q], 16);
   }
 }
 
