@@ -40,6 +40,7 @@ constexpr int SP_BIN_BITS = 11, SP_BINS = 1 << SP_BIN_BITS;
 constexpr int SP_LANE = 4, SP_SEG = SP_LANE * kWave;      // list entries of a lane and of a wave
 constexpr int SL_LANE = 16, SL_MOST = SL_LANE * kWave;    // a row's list: entries of a lane, of all
 constexpr int SL_LIST = 4 * SL_MOST;                      // the parts' shares of it are larger
+constexpr int SP_AROUND = 4;                              // bins listed on either side of a border's likely one
 constexpr int SP_SCAN = 8;                                // consecutive elements of a thread in a scan
 static_assert(SP_BINS == 2 * SP_THREADS && SP_PARTS <= SP_THREADS, "two bins a thread");
 constexpr double SP_LOG2E = 1.4426950408889634074;
@@ -924,6 +925,118 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
       double want = by_count ? static_cast<double>(a.top_k) : a.top_p * (total * fixed);
       double share = 0.0;
       if (stage == LIST) border = key_low - 1;
+      // Top-p alone: the bins' numbers of elements and mean logits (a fifth of the instructions of a
+      // weight) say nearly where its border lies.  One pass over the row then sums the weights above a few
+      // bins around it and lists those bins' elements, and the border is sought in the list; if it is not
+      // there after all, or the list is too long, the passes below find it.
+      if (by_mass && !by_count && top < __builtin_huge_valf()) {
+        for (int b = tid; b < SP_BINS; b += SP_THREADS) s.hist[b] = 0;      // (number, sum of places in the bin)
+        if (tid == 0) s.bin = 0;
+        __syncthreads();
+        row.template each<false>(wv, [&](Values v, int n, int, auto) SP_INLINE {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            if (e < n && v[e] >= cut) {
+              const int bin = linear_bin(v[e]);      // (V < 2^21 places of 2^11 steps: 32 bits)
+              const float place = (top - v[e]) * inv - static_cast<float>(SP_BINS - 1 - bin);
+              atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin]),
+                        (1ull << 32) | static_cast<uint32_t>(fminf(place, 1.0f) * 2047.0f));
+            }
+          }
+        });
+        __syncthreads();
+        {
+          const int top_bin = SP_BINS - 1 - 2 * tid;
+          double h[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const double n = static_cast<double>(s.hist[top_bin - e] >> 32);
+            const double places = static_cast<double>(static_cast<uint32_t>(s.hist[top_bin - e])) / 2047.0;
+            h[e] = n > 0.0 && inv > 0.0f ? n * pow2_or_0(-(2 * tid + e + places / n) / inv * scale, s.table) : n;
+          }
+          const double incl = wave_inclusive_scan64(h[0] + h[1]);
+          if (lane == 63) s.sum[wv] = incl;
+          __syncthreads();
+          double all;
+          const double q = waves_before(s.sum, wv, all) + incl - h[0] - h[1], aim = a.top_p * total;
+          if (q < aim && q + h[0] + h[1] >= aim) s.bin = top_bin - (q + h[0] >= aim ? 0 : 1);
+          __syncthreads();
+        }
+        // as many bins on either side as half of the list has room for (wide bins: one is enough)
+        const int middle = static_cast<int>(s.bin), side = abs(lane - SP_AROUND), at_bin = middle + lane - SP_AROUND;
+        const int near = side <= SP_AROUND && at_bin >= 0 && at_bin < SP_BINS ? static_cast<int>(s.hist[at_bin] >> 32) : 0;
+        int around = SP_AROUND;
+        while (around > 1 && wave_sum_i32(side <= around ? near : 0) > SP_WAVES * SP_SEG / 2) --around;
+        const int first = middle - around, last = middle + around;
+        uint64_t mass = 0, mass_listed = 0;
+        uint32_t key_min = 0xffffffffu, key_max = 0;
+        int n_list = 0;      // (uniform in the wave)
+        row.template each<false>(wv, [&](Values v, int n, int i, auto) SP_INLINE {
+          uint32_t on = 0;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const int bin = e < n && v[e] >= cut ? linear_bin(v[e]) : -1;
+            if (bin >= 0 && bin >= first) {
+              const double x = (static_cast<double>(v[e]) - m) * scale, w = pow2_or_0(x, s.table);
+              const uint64_t f = fixed_point(w, fixed);
+              const bool here = bin <= last;
+              on |= here ? 1u << e : 0u;
+              mass += here ? 0u : f;
+              mass_listed += here ? f : 0u;
+              sum_above += !here && x >= least ? w : 0.0;
+            }
+          }
+          if (n_list > SP_SEG || __ballot(on != 0) == 0) return;
+          const int ones = __popc(on), incl = wave_inclusive_scan_i32(ones, lane);
+          int to = n_list + incl - ones;
+          n_list += __builtin_amdgcn_readlane(incl, 63);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            if ((on >> e) & 1u) {
+              const uint32_t k = f32_order_key(v[e]);
+              key_min = min(key_min, k);
+              key_max = max(key_max, k);
+              if (to < SP_SEG) {
+                s.key[wv][to] = k;
+                s.index[wv][to] = i + e;
+              }
+              ++to;
+            }
+          }
+        });
+        mass = wave_sum64(mass);
+        mass_listed = wave_sum64(mass_listed);
+        key_min = ~wave_max_u32(~key_min);
+        key_max = wave_max_u32(key_max);
+        uint64_t sum_listed;
+        if (lane == 0) {
+          s.seg_n[wv] = n_list;
+          s.wave_mass[wv] = mass;
+          s.first[wv] = key_min;
+          s.last[wv] = key_max;
+        }
+        __syncthreads();
+        waves_before(s.wave_mass, wv, above);
+        key_min = ~wave_max_u32(lane < SP_WAVES ? ~s.first[lane] : 0u);
+        key_max = wave_max_u32(lane < SP_WAVES ? s.last[lane] : 0u);
+        have = __ballot(lane < SP_WAVES && s.seg_n[lane] > SP_SEG) == 0;
+        __syncthreads();
+        if (lane == 0) s.wave_mass[wv] = mass_listed;
+        __syncthreads();
+        waves_before(s.wave_mass, wv, sum_listed);
+        __syncthreads();
+        have = have && sum_listed > 0 && (above == 0 || static_cast<double>(above) < want) &&
+               (first <= 0 || static_cast<double>(above + sum_listed) >= want);
+        summed = have;
+        if (have) {
+          stage = KEYS;
+          lo = key_min;
+          hi = key_max;
+        } else {
+          above = 0;
+          sum_above = 0.0;
+        }
+      }
       while (by_count || by_mass) {
         if (stage == KEYS) {
           const uint32_t span = hi - lo;
