@@ -307,19 +307,24 @@ def reflex_moe_forward_timed(args: MoeArgsC, ws, events, stream=None):
 TYPE_BF16, TYPE_F32 = 0, 1
 
 
-def _codes():
+def code_types():
+    """Element types of 8-bit codes."""
     import torch
     return (torch.float8_e4m3fn, torch.uint8)
 
 
-def _want(where, name, t, dtypes, shape):
+def address(t):
+    """ptr(), and for an empty tensor (which has none) some address that nothing is read from."""
+    return None if t is None else t.data_ptr() or 256
+
+
+def want(where, name, t, dtypes, shape):
     """t: a dense tensor of one of `dtypes` and of `shape` (None: any size there)."""
-    if not isinstance(dtypes, tuple):
-        dtypes = (dtypes,)
-    if t.dtype not in dtypes:
-        raise TypeError(f"{where}: {name} has element type {t.dtype}, not {dtypes[0]}")
-    if t.dim() != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
-        raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype not in (dtypes if isinstance(dtypes, tuple) else (dtypes,)):
+        raise TypeError(f"{where}: {name} has element type {t.dtype}, not {dtypes}")
+    have = t.shape
+    if have != shape and (len(have) != len(shape) or any(w is not None and w != n for n, w in zip(have, shape))):
+        raise ValueError(f"{where}: {name} has shape {tuple(have)}, not {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{where}: {name} is not contiguous")
 
@@ -334,11 +339,13 @@ def _launch(where, tensors, args, stream):
     if device.type != "cuda":
         raise ValueError(f"{where}: tensors in device memory, not on {device}")
     fn = getattr(lib(), where)
+    # (the current stream's handle without a stream object: 0.1 us, not 2.9 of a small call's 10)
+    handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
     if device.index == torch.cuda.current_device():
-        _check(fn(*args, stream_handle(stream)), where)
+        _check(fn(*args, handle), where)
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, stream_handle(stream)), where)
+            _check(fn(*args, handle), where)
 
 
 def _pad4(k):
@@ -372,11 +379,11 @@ def reflex_select_rows(masked, rows, n_rows, ws=None, stream=None):
     import torch
     where = "reflex_select_rows"
     T = masked.shape[0]
-    _want(where, "masked", masked, (torch.uint8, torch.bool), (T,))
-    _want(where, "rows", rows, torch.int32, (T,))
-    _want(where, "n_rows", n_rows, torch.int32, (1,))
+    want(where, "masked", masked, (torch.uint8, torch.bool), (T,))
+    want(where, "rows", rows, torch.int32, (T,))
+    want(where, "n_rows", n_rows, torch.int32, (1,))
     _launch(where, (masked, rows, n_rows, ws),
-            (ptr(masked), T, ptr(rows), ptr(n_rows), ptr(ws),
+            (address(masked), T, address(rows), address(n_rows), address(ws),
              0 if ws is None else ws.numel() * ws.element_size()), stream)
 
 
@@ -384,17 +391,17 @@ def reflex_quantize_fp8(x, q, scale, rows=None, n_rows=None, stream=None):
     import torch
     where = "reflex_quantize_fp8"
     M, K = q.shape
-    _want(where, "x", x, torch.bfloat16, (None, K))
-    _want(where, "q", q, _codes(), (M, K))
-    _want(where, "scale", scale, torch.uint8, fp8_scale_shape(M, K))
+    want(where, "x", x, torch.bfloat16, (None, K))
+    want(where, "q", q, code_types(), (M, K))
+    want(where, "scale", scale, torch.uint8, fp8_scale_shape(M, K))
     if rows is not None:
-        _want(where, "rows", rows, torch.int32, (None,))
+        want(where, "rows", rows, torch.int32, (None,))
         if rows.shape[0] < M:
             raise ValueError(f"{where}: {rows.shape[0]} rows listed for {M} rows of q")
     if n_rows is not None:
-        _want(where, "n_rows", n_rows, torch.int32, (1,))
+        want(where, "n_rows", n_rows, torch.int32, (1,))
     _launch(where, (x, q, scale, rows, n_rows),
-            (ptr(x), ptr(rows), ptr(n_rows), x.shape[0], M, K, ptr(q), ptr(scale)), stream)
+            (address(x), address(rows), address(n_rows), x.shape[0], M, K, address(q), address(scale)), stream)
 
 
 def reflex_quantize_fp8_weight(w, q, scale, stream=None):
@@ -404,11 +411,11 @@ def reflex_quantize_fp8_weight(w, q, scale, stream=None):
     shape = tuple(w.shape)
     if len(shape) not in (2, 3):
         raise ValueError(f"{where}: w has shape {shape}")
-    _want(where, "w", w, torch.bfloat16, shape)
-    _want(where, "q", q, _codes(), shape)
-    _want(where, "scale", scale, torch.uint8, fp8_weight_scale_shape(*shape))
+    want(where, "w", w, torch.bfloat16, shape)
+    want(where, "q", q, code_types(), shape)
+    want(where, "scale", scale, torch.uint8, fp8_weight_scale_shape(*shape))
     E, N, K = (1,) * (3 - len(shape)) + shape
-    _launch(where, (w, q, scale), (ptr(w), E, N, K, ptr(q), ptr(scale)), stream)
+    _launch(where, (w, q, scale), (address(w), E, N, K, address(q), address(scale)), stream)
 
 
 def reflex_matmul_fp8(x, x_scale, w, w_scale, out, n_rows=None, stream=None):
@@ -416,16 +423,16 @@ def reflex_matmul_fp8(x, x_scale, w, w_scale, out, n_rows=None, stream=None):
     where = "reflex_matmul_fp8"
     M, K = x.shape
     N = w.shape[0]
-    _want(where, "x", x, _codes(), (M, K))
-    _want(where, "x_scale", x_scale, torch.uint8, fp8_scale_shape(M, K))
-    _want(where, "w", w, _codes(), (N, K))
-    _want(where, "w_scale", w_scale, torch.uint8, fp8_weight_scale_shape(N, K))
-    _want(where, "out", out, (torch.float32, torch.bfloat16), (M, N))
+    want(where, "x", x, code_types(), (M, K))
+    want(where, "x_scale", x_scale, torch.uint8, fp8_scale_shape(M, K))
+    want(where, "w", w, code_types(), (N, K))
+    want(where, "w_scale", w_scale, torch.uint8, fp8_weight_scale_shape(N, K))
+    want(where, "out", out, (torch.float32, torch.bfloat16), (M, N))
     if n_rows is not None:
-        _want(where, "n_rows", n_rows, torch.int32, (1,))
+        want(where, "n_rows", n_rows, torch.int32, (1,))
     _launch(where, (x, x_scale, w, w_scale, out, n_rows),
-            (ptr(x), ptr(x_scale), ptr(w), ptr(w_scale), ptr(n_rows), M, N, K,
-             TYPE_F32 if out.dtype == torch.float32 else TYPE_BF16, ptr(out)), stream)
+            (address(x), address(x_scale), address(w), address(w_scale), address(n_rows), M, N, K,
+             TYPE_F32 if out.dtype == torch.float32 else TYPE_BF16, address(out)), stream)
 
 
 def reflex_swiglu_fp8_workspace_size(pair_capacity, E, f) -> int:
@@ -439,20 +446,20 @@ def reflex_grouped_swiglu_fp8(h, h_scale, sorted_token, expert_offsets, w_gate, 
     T, d = h.shape
     E, f, _ = w_gate.shape
     cap = y_sorted.shape[0]
-    _want(where, "h", h, _codes(), (T, d))
-    _want(where, "h_scale", h_scale, torch.uint8, fp8_scale_shape(T, d))
-    _want(where, "sorted_token", sorted_token, torch.int32, (cap,))
-    _want(where, "expert_offsets", expert_offsets, torch.int32, (E + 1,))
+    want(where, "h", h, code_types(), (T, d))
+    want(where, "h_scale", h_scale, torch.uint8, fp8_scale_shape(T, d))
+    want(where, "sorted_token", sorted_token, torch.int32, (cap,))
+    want(where, "expert_offsets", expert_offsets, torch.int32, (E + 1,))
     for name, w, s, shape in (("gate", w_gate, s_gate, (E, f, d)), ("up", w_up, s_up, (E, f, d)),
                               ("down", w_down, s_down, (E, d, f))):
-        _want(where, "w_" + name, w, _codes(), shape)
-        _want(where, "s_" + name, s, torch.uint8, fp8_weight_scale_shape(*shape))
-    _want(where, "y_sorted", y_sorted, torch.bfloat16, (cap, d))
+        want(where, "w_" + name, w, code_types(), shape)
+        want(where, "s_" + name, s, torch.uint8, fp8_weight_scale_shape(*shape))
+    want(where, "y_sorted", y_sorted, torch.bfloat16, (cap, d))
     _launch(where, (h, h_scale, sorted_token, expert_offsets, w_gate, w_up, w_down, s_gate, s_up,
                     s_down, y_sorted, ws),
-            (ptr(h), ptr(h_scale), ptr(sorted_token), ptr(expert_offsets), ptr(w_gate), ptr(w_up),
-             ptr(w_down), ptr(s_gate), ptr(s_up), ptr(s_down), T, E, d, f, cap, ptr(y_sorted),
-             ptr(ws), ws.numel() * ws.element_size()), stream)
+            (address(h), address(h_scale), address(sorted_token), address(expert_offsets), address(w_gate), address(w_up),
+             address(w_down), address(s_gate), address(s_up), address(s_down), T, E, d, f, cap, address(y_sorted),
+             address(ws), ws.numel() * ws.element_size()), stream)
 
 
 def reflex_workspace_fp8_size(T, E, d, f, f_shared, k_max) -> int:
@@ -475,18 +482,18 @@ def reflex_sample_tokens(logits, u, params: SampleParamsC, tokens, conf=None, ro
     where = "reflex_sample_tokens"
     M, V = logits.shape
     T = tokens.shape[0]
-    _want(where, "logits", logits, (torch.float32, torch.bfloat16), (M, V))
-    _want(where, "u", u, torch.float32, (T,))
-    _want(where, "tokens", tokens, torch.int32, (T,))
+    want(where, "logits", logits, (torch.float32, torch.bfloat16), (M, V))
+    want(where, "u", u, torch.float32, (T,))
+    want(where, "tokens", tokens, torch.int32, (T,))
     if conf is not None:
-        _want(where, "conf", conf, torch.float32, (T,))
+        want(where, "conf", conf, torch.float32, (T,))
     if rows is not None:
-        _want(where, "rows", rows, torch.int32, (None,))
+        want(where, "rows", rows, torch.int32, (None,))
         if rows.shape[0] < M:
             raise ValueError(f"{where}: {rows.shape[0]} rows listed for {M} rows of logits")
     if n_rows is not None:
-        _want(where, "n_rows", n_rows, torch.int32, (1,))
+        want(where, "n_rows", n_rows, torch.int32, (1,))
     _launch(where, (logits, u, tokens, conf, rows, n_rows, ws),
-            (ptr(logits), TYPE_F32 if logits.dtype == torch.float32 else TYPE_BF16, ptr(rows),
-             ptr(n_rows), M, V, ptr(u), ctypes.byref(params), T, ptr(tokens), ptr(conf), ptr(ws),
+            (address(logits), TYPE_F32 if logits.dtype == torch.float32 else TYPE_BF16, address(rows),
+             address(n_rows), M, V, address(u), ctypes.byref(params), T, address(tokens), address(conf), address(ws),
              0 if ws is None else ws.numel() * ws.element_size()), stream)

@@ -37,6 +37,7 @@
 // gathered rows stay in L2); of a plain product the M tiles of one N tile (the weights are the
 // large operand).
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "fp8.h"
@@ -830,12 +831,15 @@ using Quarter = Shape8<1, 3, 4>;    // 64 x 256, 152 KB
 template <Mode MODE, class S, bool BIG, class OUT>
 int launch_as(const Args8& a, hipStream_t s) {
   auto* kernel = &fp8_gemm_kernel<MODE, S, BIG, OUT>;
-  static bool attr_set = false;
-  if (!attr_set) {
+  static std::atomic<uint64_t> set_on{0};      // a bit a device: the attribute is the device's own
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return REFLEX_ERR_LAUNCH;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if ((set_on.load(std::memory_order_relaxed) & bit) == 0) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                             static_cast<int>(S::LDS)) != hipSuccess)
       return REFLEX_ERR_LAUNCH;
-    attr_set = true;
+    set_on.fetch_or(bit, std::memory_order_relaxed);
   }
   const int grid = (device_cus() + G8_XCDS - 1) / G8_XCDS * G8_XCDS;      // one workgroup per CU
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::THREADS), S::LDS, s, a);

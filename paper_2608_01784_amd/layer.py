@@ -68,7 +68,7 @@ class MoELayer:
         self.norm_topk = int(norm_topk)
         self.k_rule, self.k_threshold = int(k_rule), float(k_threshold)
         self.kcap = self.uniform_k if self.uniform_k > 0 else int(params.k_max)
-        nbytes = _lib.reflex_workspace_size(T, weights.E, d, weights.f, weights.f_shared, self.kcap)
+        nbytes = self._workspace_bytes()
         if nbytes == 0 and T > 0:
             raise ValueError("unsupported layer shape")
         self.ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
@@ -76,6 +76,10 @@ class MoELayer:
         self.k = torch.empty(T, dtype=torch.int32, device=device)
         self.pairs = torch.empty(1, dtype=torch.int32, device=device)
         self.logits = torch.empty((T, weights.E), dtype=torch.float32, device=device)
+
+    def _workspace_bytes(self) -> int:
+        w = self.w
+        return _lib.reflex_workspace_size(self.T, w.E, self.d, w.f, w.f_shared, self.kcap)
 
     def args(self, h: torch.Tensor, state: Optional[TokenState] = None,
              k_in: Optional[torch.Tensor] = None, residual_a=None, residual_b=None,
@@ -112,3 +116,91 @@ class MoELayer:
 # The forward as written above: a caller that does without the method (because it has made the
 # arguments already) compares with this, so that a wrapped or replaced one is still called.
 PLAIN_FORWARD = MoELayer.forward
+
+
+def quantize_weight(w: torch.Tensor, stream=None):
+    """Codes and scales of bf16 weights [N, K] or [E, N, K] (``reflex_quantize_fp8_weight``)."""
+    q = torch.empty(w.shape, dtype=torch.float8_e4m3fn, device=w.device)
+    scale = torch.empty(_lib.fp8_weight_scale_shape(*w.shape), dtype=torch.uint8, device=w.device)
+    _lib.reflex_quantize_fp8_weight(w, q, scale, stream=stream)
+    return q, scale
+
+
+@dataclass
+class ExpertWeights8:
+    """8-bit expert weights, shapes as in ExpertWeights: codes (float8_e4m3fn or uint8) and their
+    scales (uint8, ``fp8_weight_scale_shape``); the router stays fp32."""
+    w_gate: torch.Tensor
+    w_up: torch.Tensor
+    w_down: torch.Tensor
+    s_gate: torch.Tensor
+    s_up: torch.Tensor
+    s_down: torch.Tensor
+    w_router: torch.Tensor
+    router_bias: Optional[torch.Tensor] = None
+    ws_gate: Optional[torch.Tensor] = None
+    ws_up: Optional[torch.Tensor] = None
+    ws_down: Optional[torch.Tensor] = None
+    ss_gate: Optional[torch.Tensor] = None
+    ss_up: Optional[torch.Tensor] = None
+    ss_down: Optional[torch.Tensor] = None
+
+    E = ExpertWeights.E
+    f = ExpertWeights.f
+    f_shared = ExpertWeights.f_shared
+
+    @classmethod
+    def quantize(cls, w: ExpertWeights, stream=None) -> "ExpertWeights8":
+        """The bf16 weights rounded to 8 bits (the router is shared, not copied)."""
+        made = {"w_router": w.w_router, "router_bias": w.router_bias}
+        for name in ("gate", "up", "down"):
+            made["w_" + name], made["s_" + name] = quantize_weight(getattr(w, "w_" + name), stream)
+            shared = getattr(w, "ws_" + name)
+            if shared is not None:
+                made["ws_" + name], made["ss_" + name] = quantize_weight(shared, stream)
+        return cls(**made)
+
+    def check(self, d: int):
+        """Shapes, types, density and device of all weights (the C call sees addresses alone)."""
+        where, E, f, fs = "ExpertWeights8", self.E, self.f, self.f_shared
+        sets = [("w_", "s_", (E, f, d), (E, d, f))]
+        if fs:
+            sets.append(("ws_", "ss_", (fs, d), (d, fs)))
+        for codes, scales, wide, back in sets:
+            for name, shape in (("gate", wide), ("up", wide), ("down", back)):
+                w, s = getattr(self, codes + name), getattr(self, scales + name)
+                if w is None or s is None:
+                    raise ValueError(f"{where}: {codes + name} without all of its tensors")
+                _lib.want(where, codes + name, w, _lib.code_types(), shape)
+                _lib.want(where, scales + name, s, torch.uint8, _lib.fp8_weight_scale_shape(*shape))
+                if w.device != self.w_router.device or s.device != self.w_router.device:
+                    raise ValueError(f"{where}: {codes + name} on {w.device}, the router on {self.w_router.device}")
+
+
+class MoELayer8(MoELayer):
+    """MoELayer with the experts in 8 bits (``reflex_moe_forward_fp8``): hidden states come in and go
+    out in bf16, router, counts, TopK and combine are the same."""
+
+    def __init__(self, T: int, d: int, weights: ExpertWeights8, *args, **kw):
+        weights.check(d)
+        super().__init__(T, d, weights, *args, **kw)
+        P, w = _lib.ptr, weights
+        self.experts = _lib.Fp8ExpertsC(P(w.w_gate), P(w.w_up), P(w.w_down), P(w.s_gate), P(w.s_up), P(w.s_down),
+                                        P(w.ws_gate), P(w.ws_up), P(w.ws_down), P(w.ss_gate), P(w.ss_up),
+                                        P(w.ss_down))
+
+    def _workspace_bytes(self) -> int:
+        w = self.w
+        return _lib.reflex_workspace_fp8_size(self.T, w.E, self.d, w.f, w.f_shared, self.kcap)
+
+    def args(self, *args, **kw) -> _lib.MoeArgsC:
+        a = super().args(*args, **kw)
+        a.w_gate = a.w_up = a.w_down = a.ws_gate = a.ws_up = a.ws_down = None      # (bf16 weights: not read)
+        return a
+
+    def forward(self, h, state=None, k_in=None, residual_a=None, residual_b=None, out=None,
+                stream=None) -> torch.Tensor:
+        if self.T > 0:      # (empty tensors have no address)
+            args = self.args(h, state, k_in, residual_a, residual_b, out)
+            _lib.reflex_moe_forward_fp8(args, self.experts, self.ws, stream)
+        return self.out if out is None else out
