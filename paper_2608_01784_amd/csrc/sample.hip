@@ -933,14 +933,15 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
         for (int b = tid; b < SP_BINS; b += SP_THREADS) s.hist[b] = 0;      // (number, sum of places in the bin)
         if (tid == 0) s.bin = 0;
         __syncthreads();
-        row.template each<false>(wv, [&](Values v, int n, int, auto) SP_INLINE {
+        row.template each<true>(wv, [&](Values v, int n, int, auto whole) SP_INLINE {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            if (e < n && v[e] >= cut) {
-              const int bin = linear_bin(v[e]);      // (V < 2^21 places of 2^11 steps: 32 bits)
-              const float place = (top - v[e]) * inv - static_cast<float>(SP_BINS - 1 - bin);
-              atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin]),
-                        (1ull << 32) | static_cast<uint32_t>(fminf(place, 1.0f) * 2047.0f));
+            if ((decltype(whole)::value || e < n) && v[e] >= cut) {
+              const float down = (top - v[e]) * inv;      // (as in linear_bin)
+              const int bin = static_cast<int>(fminf(down, SP_BINS - 1.0f));
+              const float place = fminf(down - static_cast<float>(bin), 1.0f);      // (V 2^11 < 2^32)
+              atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[SP_BINS - 1 - bin]),
+                        (1ull << 32) | static_cast<uint32_t>(place * 2047.0f));
             }
           }
         });
@@ -968,23 +969,31 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
         int around = SP_AROUND;
         while (around > 1 && wave_sum_i32(side <= around ? near : 0) > SP_WAVES * SP_SEG / 2) --around;
         const int first = middle - around, last = middle + around;
-        uint64_t mass = 0, mass_listed = 0;
+        // bins above the last: (top - l) inv < up_to; the listed ones and above: < list_to
+        const float up_to = static_cast<float>(SP_BINS - 1 - last);
+        const float list_to = first <= 0 ? __builtin_huge_valf() : static_cast<float>(SP_BINS - first);
+        const uint32_t by_fixed = static_cast<uint32_t>(__double_as_longlong(fixed) >> 32) - (1023u << 20);
+        const bool floored = least > -__builtin_huge_val();
+        uint64_t mass = 0;      // (a weight in fixed point as the bits of 2^52 and it)
         uint32_t key_min = 0xffffffffu, key_max = 0;
-        int n_list = 0;      // (uniform in the wave)
+        int n_list = 0, added = 0;      // (uniform in the wave)
         row.template each<false>(wv, [&](Values v, int n, int i, auto) SP_INLINE {
           uint32_t on = 0;
+          added += VEC;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            const int bin = e < n && v[e] >= cut ? linear_bin(v[e]) : -1;
-            if (bin >= 0 && bin >= first) {
-              const double x = (static_cast<double>(v[e]) - m) * scale, w = pow2_or_0(x, s.table);
-              const uint64_t f = fixed_point(w, fixed);
-              const bool here = bin <= last;
-              on |= here ? 1u << e : 0u;
-              mass += here ? 0u : f;
-              mass_listed += here ? f : 0u;
-              sum_above += !here && x >= least ? w : 0.0;
-            }
+            const float l = e < n ? v[e] : SP_NONE;
+            const float at = fmaxf(l, cut), down = (top - at) * inv;
+            const bool up = down < up_to;
+            on |= !up && down < list_to && l >= cut ? 1u << e : 0u;
+            const double d = static_cast<double>(at) - m, y = fma(d, scale, kMagic);
+            double p, t;
+            pow2_parts(y, fma(d, scale, kMagic - y), s.table, p, t);
+            u32x2_t word = __builtin_bit_cast(u32x2_t, t);      // (times the fixed point's scale; nothing below)
+            word[1] = up ? word[1] + by_fixed : 0u;
+            const double f = fma(p, __builtin_bit_cast(double, word), 0x1p52);
+            mass += static_cast<uint64_t>(__double_as_longlong(f));
+            if (floored) sum_above += up && d * scale >= least ? f - 0x1p52 : 0.0;
           }
           if (n_list > SP_SEG || __ballot(on != 0) == 0) return;
           const int ones = __popc(on), incl = wave_inclusive_scan_i32(ones, lane);
@@ -1004,6 +1013,10 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
             }
           }
         });
+        mass -= static_cast<uint64_t>(added) * 0x4330000000000000ull;
+        sum_above = (floored ? sum_above : static_cast<double>(mass)) / fixed;
+        uint64_t mass_listed = 0;      // (of the list as far as there is room for it)
+        for (int e = lane; e < min(n_list, SP_SEG); e += kWave) mass_listed += fixed_weight(s.key[wv][e]);
         mass = wave_sum64(mass);
         mass_listed = wave_sum64(mass_listed);
         key_min = ~wave_max_u32(~key_min);
