@@ -36,6 +36,14 @@
 // (workgroup b runs on XCD b % 8).  Of an expert the N tiles of one M tile are adjacent (its
 // gathered rows stay in L2); of a plain product the M tiles of one N tile (the weights are the
 // large operand).
+//
+// What bounds it, measured: many rows by the MFMAs (8192 x 8192 x 8192 2.3 PFLOP/s, where a large
+// library product of this type reaches 2.7) and, with a short K, by the tiles' stores, which come from all
+// workgroups at once and are not hidden (8192 x 8192 x 2048 2.0; 64 experts of 3 x 2048 x 1024 with 53000
+// rows 1.65); few rows by the weights' stream (48 rows of 131072 x 2048 6.2 TB/s for bf16 results, 4.8 for
+// fp32 ones; experts 3.5 to 4.5 TB/s, whose launches are short and start with two dependent
+// loads).  Letting every second workgroup start half a tile later, so that stores meet products of others, cost
+// its delay (490 -> 512 us).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -104,7 +112,7 @@ __device__ __forceinline__ int lane_here() {
   return l;
 }
 
-// ---- epilogue stores of a plain tile ---------------------------------------------------------
+// ---- epilogue stores of a tile of DOWN or PLAIN ---------------------------------------------------------
 // A wave has 32 rows x 128 columns of a pair block as four accumulators of 32 columns: lane l, register r
 // holds row l % 32 and column 8 (r/4) + 4 (l/32) + r%4.  Rows go through the wave's 4 KB of scratch in
 // LDS, 128 bytes of each at a time (64 bf16 or 32 fp32 columns), and come back with neighbouring lanes

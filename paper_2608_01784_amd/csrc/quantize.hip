@@ -1,7 +1,8 @@
 // bf16 rows and weights to 8 bits with a power-of-two scale for each block of 128 (fp8.h).
 //
 // Both kernels make one pass over the data, a block in registers between the maximum and the
-// rounding, and are bound by HBM (3 bytes a number).
+// rounding, and are bound by HBM (3 bytes a number): 8192 rows of 2048, 50 MB, 11.6 us or 4.3 TB/s,
+// where a large copy moves 5.1.
 //  - rows: a wave holds four blocks of a row (512 columns, 16 lanes and 16 bytes a lane per
 //    block), so their four scale bytes leave as one dword;
 //  - weights: a workgroup holds a 128 x 128 block, eight rows of 8 numbers in each thread.

@@ -17,12 +17,19 @@
 //     filters it holds the list in registers, finds the last kept logit of top-k and of top-p bit by
 //     bit of the 32-bit order keys (counts by ballots, weights in fixed point), and draws.
 //  4. With filters: a workgroup of 16 waves for each row whose list did not fit (flat rows, mostly of
-//     top-p).  The last kept logit is found by counts or weights in 2048 bins, first linear ones between
-//     the bound and the maximum, then over the order keys of one bin, in passes over the row (in the
-//     memory-side cache by then) until what is left fits a list in LDS.  (Fixed-point weights: the
-//     sums do not depend on the order of the atomics.)  The draw goes over the row's sixteenths and a
-//     scan of one.
+//     top-p).  For top-p alone the numbers and mean logits of 2048 linear bins say nearly where the
+//     border lies; one more pass sums the weights above that place and lists the bins around it, where the
+//     border is then sought.  Otherwise, or where that fails, the last kept logit is found by counts
+//     or weights in the bins, first linear ones between the bound and the maximum, then over the order
+//     keys of one bin, in passes over the row (in the memory-side cache by then) until what is left
+//     fits a list in LDS.  (Fixed-point weights: the sums do not depend on the order of the atomics.)  The
+//     draw goes over the row's sixteenths and a scan of one.
 // Everything is inlined and in registers: no stack.
+//
+// Measured, us (bf16 logits, temperature 1): 1024 rows of 100003 without filters 104 (launch 1: 90, bound by its
+// 32 vector instructions an element, where reading the logits takes 34), top-k 50 170, min-p 0.02 208, top-p 0.9 399 (launch 4:
+// 270 for 665 flat rows, 75 a row, bound by 50 vector instructions an element on the row's own CU); 32 rows of
+// 131072 17, 30, 66 and 112; one row of 32000 10, two launches.
 #include <algorithm>
 #include <cmath>
 #include <limits>

@@ -5,7 +5,8 @@
 // counts by a wave scan and a scan of the 16 wave sums, the chunk's indices gathered in LDS
 // and written as one contiguous run.  One chunk is one launch; more are two, the first counting
 // every chunk, the second adding up the counts before its own (at most 1024 of them) itself.
-// Bound by launch latency up to millions of positions (one read of T bytes, one write of 4 n).
+// Bound by launch latency up to millions of positions (one read of T bytes, one write of 4 n):
+// 1024 positions 2.5 us, 4.2 million 2.8 + 4.6 us.
 #include "fp8.h"
 
 namespace rfx {
