@@ -2,7 +2,7 @@
 //
 //  UP:    act[j, :] = quantize(SiLU(x_j W_gate[e]^T) * (x_j W_up[e]^T)),  x_j = h[sorted_token[j]]
 //  DOWN:  y[j, :]   = act[j, :] W_down[e]^T
-//  PLAIN: out[i, :] = x[i, :] W^T, any N, the first n_rows rows
+//  PLAIN: out[i, :] = x[i, :] W^T, any N, the first n_rows rows (fp8_slim_kernel where there are few tiles)
 // Both operands are K-contiguous codes.  Rows of one expert are contiguous; each workgroup counts
 // the experts' M tiles itself from expert_offsets, so no launch shape depends on device-resident
 // counts.  One more expert may follow the routed ones, the always-on one: every token is one of
@@ -830,25 +830,167 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   wait_copies<0>();     // the last (unused) copies land before the workgroup's LDS is released
 }
 
+// ---- plain products of few tiles -------------------------------------------------------------------
+// A product with fewer 256-column tiles than the GPU has CUs leaves most of them idle, and its time is
+// its K loop's, slice after slice.  Here a workgroup has a small tile, 32 MI rows x 32 NJ columns, and its W
+// waves take every W-th slice of K each, straight from global memory into the MFMAs' registers (whole
+// 128-byte lines of rows, SLIM_AHEAD slices ahead: nothing to share, no barrier in the loop); their sums meet in
+// LDS, added in wave order.  Bound by a load's latency: K = 4096 is four slices a wave.
+constexpr int SLIM_AHEAD = 2;
+constexpr int SLIM_PITCH = 65;      // floats between an accumulator's registers in LDS: no bank conflicts either way
+
+template <int MI, int NJ, int W, class OUT>
+__global__ __launch_bounds__(64 * W) void fp8_slim_kernel(Args8 a) {
+  constexpr bool WIDE = sizeof(OUT) == 4;
+  extern __shared__ __attribute__((aligned(16))) float slim_sums[];      // [W][MI][NJ][16][SLIM_PITCH]
+  const int K = a.K, N = a.N, nk = K / G8_BK, groups = (nk + 3) / 4;
+  int rows = a.sh_rows;
+  if (a.n_rows != nullptr) rows = min(max(a.n_rows[0], 0), rows);
+  const int m_tiles = (a.sh_rows + 32 * MI - 1) / (32 * MI);
+  const int row0 = static_cast<int>(blockIdx.x) % m_tiles * 32 * MI, n0 = static_cast<int>(blockIdx.x) / m_tiles * 32 * NJ;
+  if (row0 >= rows) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (rows and columns past the last are the last one's again, and not stored)
+  const uint8_t *x[MI], *w[NJ];
+  const uint32_t *xs[MI], *ws[NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = min(row0 + 32 * i + lane % 32, rows - 1);
+    x[i] = a.x + static_cast<size_t>(r) * K + 32 * (lane / 32);
+    xs[i] = a.x_scale + r;
+  }
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int n = min(n0 + 32 * j + lane % 32, N - 1);
+    w[j] = a.sw0 + static_cast<size_t>(n) * K + 32 * (lane / 32);
+    ws[j] = a.ss0 + static_cast<size_t>(min(n0 + 32 * j, N - 1) / F8_BLOCK) * groups;
+  }
+  // A slice: lane l has bytes 32 (l / 32) .. of each half of its rows' 128 (of both operands alike)
+  struct Slice {
+    i32x4_t x[MI][4], w[NJ][4];
+    uint32_t sx[MI], sw[NJ];
+  } slice[SLIM_AHEAD];
+  auto load = [&](Slice& f, int k) {
+    k = min(k, nk - 1);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        f.x[i][q] = *reinterpret_cast<const i32x4_t*>(x[i] + static_cast<size_t>(k) * G8_BK + 64 * (q / 2) + 16 * (q % 2));
+      f.sx[i] = xs[i][static_cast<size_t>(k >> 2) * a.x_rows];
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        f.w[j][q] = *reinterpret_cast<const i32x4_t*>(w[j] + static_cast<size_t>(k) * G8_BK + 64 * (q / 2) + 16 * (q % 2));
+      f.sw[j] = ws[j][k >> 2];
+    }
+  };
+  f32x16_t acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16_t{};
+  auto multiply = [&](const Slice& f, int k) {
+    const int shift = 8 * (k & 3);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const uint32_t sx = (f.sx[i] >> shift) & 0xffu, sw = (f.sw[j] >> shift) & 0xffu;
+          if constexpr (WIDE) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const i32x4_t &xv = f.x[i][2 * kk + q / 2], &wv = f.w[j][2 * kk + q / 2];
+              const int at = 2 * (q % 2);
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(wv[at], wv[at + 1], __uint_as_float(sw << 23)),
+                                                                  widen8(xv[at], xv[at + 1], __uint_as_float(sx << 23)),
+                                                                  acc[i][j], 0, 0, 0);
+            }
+          } else {
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                __builtin_shufflevector(f.w[j][2 * kk], f.w[j][2 * kk + 1], 0, 1, 2, 3, 4, 5, 6, 7),
+                __builtin_shufflevector(f.x[i][2 * kk], f.x[i][2 * kk + 1], 0, 1, 2, 3, 4, 5, 6, 7), acc[i][j], 0, 0, 0,
+                static_cast<int>(sw), 0, static_cast<int>(sx));
+          }
+        }
+  };
+  if (wave < nk) {
+#pragma unroll
+    for (int d = 0; d < SLIM_AHEAD; ++d) load(slice[d], wave + d * W);
+    for (int k = wave; k < nk; k += SLIM_AHEAD * W) {
+#pragma unroll
+      for (int d = 0; d < SLIM_AHEAD; ++d) {
+        if (k + d * W < nk) multiply(slice[d], k + d * W);
+        if (k + (d + SLIM_AHEAD) * W < nk) load(slice[d], k + (d + SLIM_AHEAD) * W);
+      }
+    }
+  }
+  // lane l, register r: row l % 32, column 8 (r / 4) + 4 (l / 32) + r % 4
+  auto sums = [&](int v, int i, int j) { return slim_sums + ((v * MI + i) * NJ + j) * 16 * SLIM_PITCH; };
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sums(wave, i, j)[r * SLIM_PITCH + lane] = acc[i][j][r];
+  __syncthreads();
+  OUT* const out = static_cast<OUT*>(a.out);
+  for (int t = threadIdx.x; t < 1024 * MI * NJ; t += 64 * W) {      // neighbouring threads: neighbouring columns
+    const int col = t % (32 * NJ), row = t / (32 * NJ), c = col % 32;
+    if (row0 + row >= rows || n0 + col >= N) continue;
+    const float* const at = sums(0, row / 32, col / 32) + ((c / 8) * 4 + c % 4) * SLIM_PITCH + row % 32 + 32 * ((c / 4) % 2);
+    float sum = at[0];
+#pragma unroll
+    for (int v = 1; v < W; ++v) sum += at[v * MI * NJ * 16 * SLIM_PITCH];
+    if constexpr (WIDE)
+      out[static_cast<size_t>(row0 + row) * N + n0 + col] = sum;
+    else
+      out[static_cast<size_t>(row0 + row) * N + n0 + col] = f32_to_bf16(sum);
+  }
+}
+
 // The tile shapes (pair rows x weight rows).  The activation's blocks of 128 columns need 256
 // weight rows a tile (128 of gate, 128 of up).
 using Tall = Shape8<4, 2, 3>;       // 256 x 256, 160 KB of LDS, one workgroup per CU
 using Half = Shape8<2, 3, 3>;       // 128 x 256, 144 KB
 using Quarter = Shape8<1, 3, 4>;    // 64 x 256, 152 KB
 
-template <Mode MODE, class S, bool BIG, class OUT>
-int launch_as(const Args8& a, hipStream_t s) {
-  auto* kernel = &fp8_gemm_kernel<MODE, S, BIG, OUT>;
-  static std::atomic<uint64_t> set_on{0};      // a bit a device: the attribute is the device's own
+// Lets a kernel have `lds` bytes of LDS; set_on: a bit a device (the attribute is the device's own).
+int allow_lds(const void* kernel, size_t lds, std::atomic<uint64_t>& set_on) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return REFLEX_ERR_LAUNCH;
   const uint64_t bit = uint64_t(1) << (dev & 63);
   if ((set_on.load(std::memory_order_relaxed) & bit) == 0) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            static_cast<int>(S::LDS)) != hipSuccess)
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds)) != hipSuccess)
       return REFLEX_ERR_LAUNCH;
     set_on.fetch_or(bit, std::memory_order_relaxed);
   }
+  return REFLEX_OK;
+}
+
+template <int MI, int NJ, int W, class OUT>
+int launch_slim(const Args8& a, hipStream_t s) {
+  constexpr size_t lds = sizeof(float) * W * MI * NJ * 16 * SLIM_PITCH;
+  static_assert(lds <= 160 * 1024, "LDS");
+  auto* kernel = &fp8_slim_kernel<MI, NJ, W, OUT>;
+  static std::atomic<uint64_t> set_on{0};
+  const int rc = allow_lds(reinterpret_cast<const void*>(kernel), lds, set_on);
+  if (rc != REFLEX_OK) return rc;
+  const int tiles = (a.sh_rows + 32 * MI - 1) / (32 * MI) * ((a.N + 32 * NJ - 1) / (32 * NJ));
+  hipLaunchKernelGGL(kernel, dim3(tiles), dim3(64 * W), lds, s, a);
+  return launch_status();
+}
+
+template <Mode MODE, class S, bool BIG, class OUT>
+int launch_as(const Args8& a, hipStream_t s) {
+  auto* kernel = &fp8_gemm_kernel<MODE, S, BIG, OUT>;
+  static std::atomic<uint64_t> set_on{0};
+  const int rc = allow_lds(reinterpret_cast<const void*>(kernel), S::LDS, set_on);
+  if (rc != REFLEX_OK) return rc;
   const int grid = (device_cus() + G8_XCDS - 1) / G8_XCDS * G8_XCDS;      // one workgroup per CU
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::THREADS), S::LDS, s, a);
   return launch_status();
@@ -862,6 +1004,15 @@ int launch_as(const Args8& a, hipStream_t s) {
 // 182 / 169 / 134, 512 rows 285 / 230 / 220.
 template <Mode MODE, class OUT>
 int launch_gemm8(const Args8& a, int rows, hipStream_t s) {
+  if constexpr (MODE == PLAIN) {
+    // Small tiles while they find a CU each (32 x 32: two to a CU).  2048 columns of K, bf16 / fp32 results, us:
+    // 16 x 4096 9.8 / 9.9 in 32 x 32 tiles, 12.7 / 18.1 in 64 x 256; 256 x 2048 11.6 / 10.9, in 64 x 64 12.6 / 13.3,
+    // in 256 x 256 26.8 / 46.6; 1024 x 1024 20.6 / 18.4, 12.8 / 14.1, 27.0 / 46.7; 64 x 16384 21.7 / 18.3, 13.2 / 14.4,
+    // 15.4 / 21.9; 64 x 24576 31.5 / 25.4, 24.2 / 25.8, 15.7 / 22.8.
+    const auto tiles = [&](int side) { return static_cast<long long>((rows + side - 1) / side) * ((a.N + side - 1) / side); };
+    if (tiles(32) <= 2 * device_cus()) return launch_slim<1, 1, 8, OUT>(a, s);
+    if (tiles(64) <= device_cus()) return launch_slim<2, 2, 4, OUT>(a, s);
+  }
   if (static_cast<size_t>(a.x_rows) * static_cast<size_t>(a.K) >= (size_t(1) << 31))
     return launch_as<MODE, Tall, true, OUT>(a, s);
   if (rows <= Quarter::BM) return launch_as<MODE, Quarter, false, OUT>(a, s);

@@ -200,6 +200,28 @@ def test_product(torch, lib, M, N, K, out):
     note(f"product {M} x {N} x {K} {out}: {worst:.3f} of the bound")
 
 
+# (products of few 256-column tiles have a kernel of their own: these have many)
+@pytest.mark.parametrize("M, N, K", [(1, 16500, 128), (33, 16641, 256), (64, 20003, 640), (70, 17003, 384), (128, 16392, 1152),
+                                     (129, 16400, 512), (300, 33001, 128), (513, 8450, 256)])
+@pytest.mark.parametrize("out", ["float32", "bfloat16"])
+def test_product_of_many_columns(torch, lib, M, N, K, out):
+    x, xs, w, ws = product_case(torch, lib, M, N, K)
+    y = torch.full((M, N), float("nan"), dtype=getattr(torch, out), device="cuda")
+    lib.reflex_matmul_fp8(x, xs, w, ws, y)
+    check_product(f64(y), x, xs, w, ws, 0.0 if out == "float32" else 2.0 ** -8)
+
+
+@pytest.mark.parametrize("used", [0, 1, 64, 65, 129, 399, 400, 1000])
+def test_product_of_counted_rows_and_many_columns(torch, lib, used):
+    x, xs, w, ws = product_case(torch, lib, 400, 16897, 256)
+    y = torch.full((400, 16897), 5.0, device="cuda")
+    lib.reflex_matmul_fp8(x, xs, w, ws, y, n_rows=torch.tensor([used], dtype=torch.int32, device="cuda"))
+    n = min(used, 400)
+    assert (y[n:] == 5.0).all()
+    if n:
+        check_product(f64(y[:n]), x[:n], xs[:, :n].contiguous(), w, ws, 0.0)
+
+
 @pytest.mark.parametrize("M, used", [(70, 0), (70, 1), (70, 64), (70, 69), (70, 70), (70, 500), (70, -1), (400, 129), (400, 3)])
 def test_product_of_counted_rows(torch, lib, M, used):
     N, K = 201, 640
