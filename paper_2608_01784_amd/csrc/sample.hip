@@ -440,21 +440,51 @@ __global__ __launch_bounds__(SS_THREADS) void sample_list_kernel(const E* __rest
   if (lane == 0) a.listed[static_cast<size_t>(j) * a.parts + p] = n_list > room ? -1 : n_list;
 }
 
+// A row's parts, lane l with parts l, l + 64, .. (none: nothing of them), loaded together: a row's launch is a
+// chain of loads from other launches' results, 1 us each.
+constexpr int SP_PARTS_LANE = (SP_PARTS + kWave - 1) / kWave;
+struct RowParts {
+  double sum[SP_PARTS_LANE], flat[SP_PARTS_LANE];
+  float top[SP_PARTS_LANE];
+  int first[SP_PARTS_LANE];
+};
+RFX_DEVICE RowParts load_parts(const SampleArgs& a, const Part* part) {
+  RowParts r;
+#pragma unroll
+  for (int q = 0; q < SP_PARTS_LANE; ++q) {
+    const int p = kWave * q + static_cast<int>(threadIdx.x & 63);
+    r.sum[q] = r.flat[q] = 0.0;
+    r.top[q] = SP_NONE;
+    r.first[q] = 0x7fffffff;
+    if (p < a.parts) {
+      r.sum[q] = part[p].sum;
+      r.flat[q] = part[p].flat;
+      r.top[q] = part[p].top;
+      r.first[q] = part[p].first;
+    }
+  }
+  return r;
+}
+
 // A row's sums from its parts', by one wave; first: the maximum's first index.
-RFX_DEVICE void row_flat(const SampleArgs& a, const Part* part, const double* table, float& top, int& first,
+RFX_DEVICE void row_flat(const SampleArgs& a, const RowParts& part, const double* table, float& top, int& first,
                          double& total, double& flat) {
-  const int lane = threadIdx.x & 63;
   uint64_t most = 0;
-  for (int p = lane; p < a.parts; p += kWave)
-    most = max(most, (static_cast<uint64_t>(f32_order_key(part[p].top)) << 32) | (0x7fffffffu - static_cast<uint32_t>(part[p].first)));
+#pragma unroll
+  for (int q = 0; q < SP_PARTS_LANE; ++q)
+    if (kWave * q < a.parts)
+      most = max(most, (static_cast<uint64_t>(f32_order_key(part.top[q])) << 32) | (0x7fffffffu - static_cast<uint32_t>(part.first[q])));
   most = wave_max_u64(most);
   top = f32_from_order_key(static_cast<uint32_t>(most >> 32));
   first = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(most));
   total = flat = 0.0;
-  for (int p = lane; p < a.parts; p += kWave) {
-    const double down = static_cast<double>(part[p].top) - static_cast<double>(top);
-    total += part[p].sum * pow2_or_0(down * a.scale, table);
-    flat += part[p].flat * pow2_or_0(down * SP_LOG2E, table);
+#pragma unroll
+  for (int q = 0; q < SP_PARTS_LANE; ++q) {
+    if (kWave * q < a.parts) {
+      const double down = static_cast<double>(part.top[q]) - static_cast<double>(top);
+      total += part.sum[q] * pow2_or_0(down * a.scale, table);
+      flat += part.flat[q] * pow2_or_0(down * SP_LOG2E, table);
+    }
   }
   total = wave_sum64(total);
   flat = a.scale == SP_LOG2E ? total : wave_sum64(flat);
@@ -475,18 +505,25 @@ __global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restr
   __shared__ double table[64];
   __shared__ int s_at[SS_WAVES][SP_PARTS + 1];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + wv), V = a.V, parts = a.parts;
+  // (loads of a row of the workspace, ahead of what decides whether there is such a row)
+  const size_t row_of = static_cast<size_t>(min(j, a.M - 1)) * parts;
+  const Part* const part = a.part + row_of;
+  const RowParts of_row = load_parts(a, part);
+  int listed[SP_PARTS_LANE];
+#pragma unroll
+  for (int q = 0; q < SP_PARTS_LANE; ++q)
+    listed[q] = FILTERS && kWave * q + lane < parts ? a.listed[row_of + kWave * q + lane] : 0;
   if (tid < 64) table[tid] = pow2_entry(tid);
   __syncthreads();
-  const int j = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + wv), V = a.V, parts = a.parts;
   if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
   const int pos = a.rows == nullptr ? j : a.rows[j];
   if (pos < 0 || pos >= a.T) return;
-  const Part* const part = a.part + static_cast<size_t>(j) * parts;
   const Row<E> row(logits + static_cast<size_t>(j) * V, V, parts);
   float top;
   int token;
   double total, flat;
-  row_flat(a, part, table, top, token, total, flat);
+  row_flat(a, of_row, table, top, token, total, flat);
   float u = a.u[pos];
   u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
   const double m = top, scale = a.scale;
@@ -518,15 +555,17 @@ __global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restr
     }
   } else if (FILTERS) {
     // the list, lane l's entries R l .. R l + R - 1 of it
-    const int32_t* const listed = a.listed + static_cast<size_t>(j) * parts;
     int all = 0;
     bool fits = true;
-    for (int p0 = 0; p0 < parts; p0 += kWave) {
-      const int n = p0 + lane < parts ? listed[p0 + lane] : 0;
-      fits = fits && __ballot(n < 0) == 0;
-      const int incl = wave_inclusive_scan_i32(n, lane);
-      if (p0 + lane < parts) s_at[wv][p0 + lane] = all + incl - n;
-      all += __builtin_amdgcn_readlane(incl, 63);
+#pragma unroll
+    for (int q = 0; q < SP_PARTS_LANE; ++q) {
+      if (kWave * q < parts) {
+        const int n = listed[q], p = kWave * q + lane;
+        fits = fits && __ballot(n < 0) == 0;
+        const int incl = wave_inclusive_scan_i32(n, lane);
+        if (p < parts) s_at[wv][p] = all + incl - n;
+        all += __builtin_amdgcn_readlane(incl, 63);
+      }
     }
     if (!fits || all > SL_MOST) return;      // the fourth launch's
     if (lane == 0) s_at[wv][parts] = all;
@@ -767,7 +806,7 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
   float top;
   int token;
   double total, flat;
-  row_flat(a, part_of, s.table, top, token, total, flat);
+  row_flat(a, load_parts(a, part_of), s.table, top, token, total, flat);
   const double m = top;
   const uint32_t key_top = f32_order_key(top);
   auto power = [&](uint32_t k) SP_INLINE { return (static_cast<double>(f32_from_order_key(k)) - m) * scale; };
@@ -936,7 +975,8 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
       // weight) say nearly where its border lies.  One pass over the row then sums the weights above a few
       // bins around it and lists those bins' elements, and the border is sought in the list; if it is not
       // there after all, or the list is too long, the passes below find it.
-      if (by_mass && !by_count && top < __builtin_huge_valf()) {
+      // (Rows that fit the list whole need no such search.)
+      if (by_mass && !by_count && V > SP_WAVES * SP_SEG && top < __builtin_huge_valf()) {
         for (int b = tid; b < SP_BINS; b += SP_THREADS) s.hist[b] = 0;      // (number, sum of places in the bin)
         if (tid == 0) s.bin = 0;
         __syncthreads();
