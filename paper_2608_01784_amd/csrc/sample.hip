@@ -601,6 +601,15 @@ __global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restr
     least = ~wave_max_u32(~least);
     const int bits = least == key_top ? 0 : 32 - __builtin_clz(least ^ key_top);      // that differ
     const uint32_t common = bits == 32 ? 0u : key_top >> bits << bits;
+    // A lane's entries, four at a time (those past the list have key 0, below every key that is tried).
+    auto each_listed = [&](auto&& f) SP_INLINE {
+#pragma unroll
+      for (int r0 = 0; r0 < SL_LANE; r0 += 4)
+        if (r0 < R) {
+#pragma unroll
+          for (int r = r0; r < r0 + 4; ++r) f(r);
+        }
+    };
     uint32_t border = 0;
     int ties = 0x7fffffff;
     if (by_count && a.top_k < all) {
@@ -609,16 +618,12 @@ __global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restr
         const uint32_t t = border | (1u << bit);
         if (t > key_top) continue;
         int n = 0;
-#pragma unroll
-        for (int r = 0; r < SL_LANE; ++r)
-          if (r < R) n += __popcll(__ballot(key[r] >= t));
-        if (n >= a.top_k) border = t;
+        each_listed([&](int r) SP_INLINE { n += key[r] >= t ? 1 : 0; });
+        if (wave_sum_i32(n) >= a.top_k) border = t;
       }
       int above = 0;
-#pragma unroll
-      for (int r = 0; r < SL_LANE; ++r)
-        if (r < R) above += __popcll(__ballot(key[r] > border));
-      ties = a.top_k - above;
+      each_listed([&](int r) SP_INLINE { above += key[r] > border ? 1 : 0; });
+      ties = a.top_k - wave_sum_i32(above);
     }
     // Of what is equal to `border`, this lane's first's rank.
     auto tie_rank = [&]() SP_INLINE {
@@ -646,15 +651,14 @@ __global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restr
         sum += q[r];
       }
       const double want = a.top_p * (by_count ? static_cast<double>(wave_sum64(sum)) : total * fixed);
+      const uint64_t least_sum = static_cast<uint64_t>(ceil(want));      // (below 2^52)
       uint32_t last = common;      // the largest key from which on the weights sum to `want`
       for (int bit = bits - 1; bit >= 0; --bit) {
         const uint32_t t = last | (1u << bit);
         if (t > key_top) continue;
         sum = 0;
-#pragma unroll
-        for (int r = 0; r < SL_LANE; ++r)
-          if (r < R) sum += key[r] >= t ? q[r] : 0;
-        if (static_cast<double>(wave_sum64(sum)) >= want) last = t;
+        each_listed([&](int r) SP_INLINE { sum += key[r] >= t ? q[r] : 0; });
+        if (wave_sum64(sum) >= least_sum) last = t;
       }
       uint64_t above = 0;
 #pragma unroll
