@@ -326,3 +326,21 @@ def test_experts(torch, lib, T, d, f, sizes, extra):
 def test_experts_without_rows(torch, lib):
     c = expert_case(torch, lib, 4, 128, 128, [0, 0], 3)
     assert (run_experts(torch, lib, c) == 5.0).all()
+
+
+@pytest.mark.parametrize("T, d, f, sizes", [(20, 256, 256, [9, 0, 11]), (90, 256, 128, [70, 60]), (300, 384, 256, [300])])
+def test_experts_keep_what_is_not_finite_in_its_row(torch, lib, T, d, f, sizes):
+    """Rows of NaN, and rows whose activation overflows in some columns: their results are NaN, all others
+    within the bound."""
+    c = expert_case(torch, lib, T, d, f, sizes)
+    c["token"] = (np.arange(c["cap"]) % T).astype(np.int32)
+    bad = [3 % T, T // 2]
+    c["h"][bad[0], 5] = 0x7f
+    c["hs"][:, bad[1]] = 247      # (2^120: the product of gate and up is past fp32)
+    y = f64(run_experts(torch, lib, c))
+    hit = np.isin(c["token"][:c["P"]], bad)
+    assert np.isnan(y[:c["P"]][hit]).all()
+    good = dict(c, token=c["token"][:c["P"]][~hit], P=int((~hit).sum()))
+    owner = np.repeat(np.arange(len(sizes)), sizes)[~hit]
+    good["offsets"] = np.searchsorted(owner, np.arange(len(sizes) + 1)).astype(np.int32)
+    check_experts(good, torch.from_numpy(np.concatenate([y[:c["P"]][~hit], y[c["P"]:]])))

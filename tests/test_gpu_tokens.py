@@ -188,3 +188,22 @@ def test_confidence_is_optional(torch, lib):
     lib.reflex_sample_tokens(x, u, p, a, ws=ws)
     lib.reflex_sample_tokens(x, u, p, b, torch.empty(4, device="cuda"), ws=ws)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("params", [(1.0, 0, 0.9, 0.0), (1.5, 0, 0.5, 0.01), (1.0, 5000, 0.7, 0.0), (1.0, 0, 1.0, 0.05)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_flat_rows_of_every_order(torch, lib, dtype, params):
+    """Rows in which the tokens around a border lie together, repeat, or are few: ascending, descending, of
+    five values, with one token far above the others, with two levels, and next to the border of a wave's share."""
+    V = 40013
+    rng = np.random.default_rng(V)
+    x = rng.normal(size=(6, V)) * 2.0
+    x[0], x[1] = np.sort(x[0]), -np.sort(x[1])
+    x[2] = np.round(x[2] / 2.0)
+    x[3, 777] = 12.0
+    x[4] = np.where(rng.random(V) < 0.3, 1.0, 0.0)
+    x[5] = np.where(np.arange(V) % 2501 < 40, 3.0, 0.0) + 1e-3 * x[5]
+    dev = torch.from_numpy(x.astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    for k in range(3):
+        u = rng.random(6, dtype=np.float32)
+        check(dev.double().cpu().numpy(), u, params, *sample(torch, lib, dev, u, params))
