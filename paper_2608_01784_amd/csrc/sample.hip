@@ -81,6 +81,7 @@ struct SampleArgs {
   int32_t* tokens;
   float* conf;
   Part* part;            // [M, parts]
+  float* pair;           // [M, parts, 32]: maxima of the pairs of lanes
   int32_t* listed;       // [M, parts]: the parts' numbers of listed elements, -1 for too many
   Listed* list;          // [M, SP_LIST]: parts' shares one after the other
 };
@@ -243,7 +244,8 @@ struct Row {
   }
 };
 
-template <class E, bool DRAWS, bool FLAT>      // FLAT: the confidence's sum is another one than the weights'
+// FLAT: the confidence's sum is another one than the weights'.  PAIRS: top-k, whose bound may want the pairs' maxima.
+template <class E, bool DRAWS, bool FLAT, bool PAIRS>
 __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __restrict__ logits, SampleArgs a) {
   constexpr int VEC = Row<E>::VEC;
   using Values = typename Row<E>::Values;
@@ -299,11 +301,6 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
     }
     if (FLAT) flat += static_cast<double>(z);
   });
-  // maxima of the groups of eight lanes (no elements: -inf)
-  uint32_t group = f32_order_key(best);
-  group = max(group, dpp_u32<kDppXor1>(group));
-  group = max(group, dpp_u32<kDppXor2>(group));
-  group = max(group, dpp_u32<kDppHalfMirror>(group));
   const uint64_t key =
       wave_max_u64((static_cast<uint64_t>(f32_order_key(best)) << 32) | (0x7fffffffu - static_cast<uint32_t>(at)));
   const float top = f32_from_order_key(static_cast<uint32_t>(key >> 32));
@@ -311,19 +308,26 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
   if (DRAWS) sum = wave_sum64(sum * pow2_or_0(down * scale, table));
   if (FLAT) flat = wave_sum64(flat * exp2(down * SP_LOG2E));
   if (top == SP_NONE) sum = flat = 0.0;
-  Part* const out = a.part + static_cast<size_t>(j) * a.parts + part;
+  Part* const out = a.part + item;
   if (lane == 0) {
     out->sum = sum;
     out->flat = flat;
     out->top = top;
     out->first = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(key));
   }
+  // maxima of the pairs and of the groups of eight lanes (no elements: -inf)
+  uint32_t group = f32_order_key(best);
+  group = max(group, dpp_u32<kDppXor1>(group));
+  if (PAIRS && lane % 2 == 0) (a.pair + static_cast<size_t>(item) * (kWave / 2))[static_cast<uint32_t>(lane) / 2] = f32_from_order_key(group);
+  group = max(group, dpp_u32<kDppXor2>(group));
+  group = max(group, dpp_u32<kDppHalfMirror>(group));
   if (lane % 8 == 0) out->group[lane / 8] = f32_from_order_key(group);
 }
 
 // The bound of a row's filters, by one wave: no kept logit lies below it.
 //  - Top-k: as many groups of lanes as have elements have a maximum each; top_k of them are at least
-//    the bound (its key's low 16 bits zero), so top_k elements are.
+//    the bound (its key's low 16 bits zero), so top_k elements are.  Of G groups of random elements some
+//    G ln(G / (G - top_k)) elements lie above; pairs serve where the groups of eight lanes are too few.
 //  - Top-p: the tokens of less than the share (1 - top_p) / V together weigh less than what may be left
 //    out.
 //  - Min-p itself; not where top-p needs the weight of what top-k leaves, min-p's part among it.
@@ -349,23 +353,33 @@ RFX_DEVICE float filter_bound(const SampleArgs& a, const Part* part, double m, d
       if (n >= a.top_k) bound = t;
     }
     if (bound > f32_order_key(SP_LOWEST)) cut = f32_from_order_key(bound);
-  } else if (by_count && a.top_k <= groups) {
-    uint32_t bound = 0;
-    uint32_t key[8 * SP_PARTS / kWave];
+  } else if (by_count) {
+    // the top_k-th of n entries, if they are enough
+    auto bound_of = [&](int n_entries, auto&& entry) SP_INLINE {
+      if (a.top_k > n_entries) return;
+      uint32_t bound = 0;
+      uint32_t key[8 * SP_PARTS / kWave];
 #pragma unroll
-    for (int q = 0; q < 8 * SP_PARTS / kWave; ++q) {
-      const int g = q * kWave + lane;
-      key[q] = g < groups ? f32_order_key(part[g / 8].group[g % 8]) : 0u;
-    }
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t t = bound | (1u << bit);
-      int n = 0;
+      for (int q = 0; q < 8 * SP_PARTS / kWave; ++q) {
+        const int g = q * kWave + lane;
+        key[q] = g < n_entries ? f32_order_key(entry(g)) : 0u;
+      }
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t t = bound | (1u << bit);
+        int n = 0;
 #pragma unroll
-      for (int q = 0; q < 8 * SP_PARTS / kWave; ++q)
-        if (q * kWave < groups) n += __popcll(__ballot(key[q] >= t));
-      if (n >= a.top_k) bound = t;
+        for (int q = 0; q < 8 * SP_PARTS / kWave; ++q)
+          if (q * kWave < n_entries) n += __popcll(__ballot(key[q] >= t));
+        if (n >= a.top_k) bound = t;
+      }
+      if (bound > f32_order_key(SP_LOWEST)) cut = f32_from_order_key(bound);
+    };
+    if (8 * a.top_k <= 7 * groups || a.parts > SP_PARTS / 4) {
+      bound_of(groups, [&](int g) SP_INLINE { return part[g / 8].group[g % 8]; });
+    } else {
+      const float* const pair = a.pair + (part - a.part) * (kWave / 2);
+      bound_of(kWave / 2 * a.parts, [&](int g) SP_INLINE { return pair[g]; });
     }
-    if (bound > f32_order_key(SP_LOWEST)) cut = f32_from_order_key(bound);
   } else if (!by_count && by_mass) {
     cut = static_cast<float>(m + (log2((1.0 - a.top_p) * total / a.V) - 0.001) / a.scale);
   }
@@ -1327,22 +1341,26 @@ int parts_of(int M, int V) {
 
 static bool filters(const SampleArgs& a) { return a.top_k < a.V || a.top_p < 1.0 || a.floor2 > -1.0e300; }
 
-// The parts' records, then the numbers of elements listed, then the lists.
+// The parts' records, the numbers of elements listed, the maxima of pairs, the lists.
 static size_t part_bytes(int M, int V) { return align_up(sizeof(Part) * static_cast<size_t>(M) * parts_of(M, V)); }
 static size_t listed_bytes(int M, int V) { return align_up(sizeof(int32_t) * static_cast<size_t>(M) * parts_of(M, V)); }
+static size_t pair_bytes(int M, int V) {
+  return align_up(sizeof(float) * (kWave / 2) * static_cast<size_t>(M) * parts_of(M, V));
+}
 size_t sample_ws_bytes(int M, int V) {
-  return part_bytes(M, V) + listed_bytes(M, V) + align_up(sizeof(Listed) * static_cast<size_t>(M) * SL_LIST);
+  return part_bytes(M, V) + listed_bytes(M, V) + pair_bytes(M, V) + align_up(sizeof(Listed) * static_cast<size_t>(M) * SL_LIST);
 }
 
 template <class E>
 static int launch_sample_as(const E* logits, const SampleArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((static_cast<size_t>(a.M) * a.parts + SS_WAVES - 1) / SS_WAVES));
-  if (a.scale == SP_LOG2E)
-    hipLaunchKernelGGL((sample_sums_kernel<E, true, false>), grid, dim3(SS_THREADS), 0, s, logits, a);
-  else if (a.scale > 0.0)
-    hipLaunchKernelGGL((sample_sums_kernel<E, true, true>), grid, dim3(SS_THREADS), 0, s, logits, a);
+  auto sums = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(SS_THREADS), 0, s, logits, a); };
+  if (a.scale == 0.0)
+    sums(sample_sums_kernel<E, false, true, false>);
+  else if (a.scale == SP_LOG2E)
+    a.top_k < a.V ? sums(sample_sums_kernel<E, true, false, true>) : sums(sample_sums_kernel<E, true, false, false>);
   else
-    hipLaunchKernelGGL((sample_sums_kernel<E, false, true>), grid, dim3(SS_THREADS), 0, s, logits, a);
+    a.top_k < a.V ? sums(sample_sums_kernel<E, true, true, true>) : sums(sample_sums_kernel<E, true, true, false>);
   const dim3 rows(static_cast<unsigned>((a.M + SS_WAVES - 1) / SS_WAVES));
   if (a.scale > 0.0 && filters(a)) {
     hipLaunchKernelGGL((sample_list_kernel<E>), grid, dim3(SS_THREADS), 0, s, logits, a);
@@ -1357,12 +1375,16 @@ static int launch_sample_as(const E* logits, const SampleArgs& a, hipStream_t s)
 int launch_sample(const void* logits, int logits_type, const int32_t* rows, const int32_t* n_rows, int M, int V,
                   const float* u, const reflex_sample_params& p, int T, int32_t* tokens, float* conf, void* ws,
                   hipStream_t s) {
+  char* at[4] = {static_cast<char*>(ws)};
+  at[1] = at[0] + part_bytes(M, V);
+  at[2] = at[1] + listed_bytes(M, V);
+  at[3] = at[2] + pair_bytes(M, V);
   const SampleArgs a{rows, n_rows, M, V, T, parts_of(M, V), u,
                      p.temperature > 0.0f ? SP_LOG2E / static_cast<double>(p.temperature) : 0.0,
                      p.min_p > 0.0f ? std::log2(static_cast<double>(p.min_p)) : -std::numeric_limits<double>::infinity(),
                      p.top_k > 0 && p.top_k < V ? p.top_k : V, static_cast<double>(p.top_p), tokens, conf,
-                     static_cast<Part*>(ws), reinterpret_cast<int32_t*>(static_cast<char*>(ws) + part_bytes(M, V)),
-                     reinterpret_cast<Listed*>(static_cast<char*>(ws) + part_bytes(M, V) + listed_bytes(M, V))};
+                     reinterpret_cast<Part*>(at[0]), reinterpret_cast<float*>(at[2]), reinterpret_cast<int32_t*>(at[1]),
+                     reinterpret_cast<Listed*>(at[3])};
   return logits_type == REFLEX_TYPE_F32 ? launch_sample_as(static_cast<const float*>(logits), a, s)
                                         : launch_sample_as(static_cast<const uint16_t*>(logits), a, s);
 }

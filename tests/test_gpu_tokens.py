@@ -207,3 +207,16 @@ def test_flat_rows_of_every_order(torch, lib, dtype, params):
     for k in range(3):
         u = rng.random(6, dtype=np.float32)
         check(dev.double().cpu().numpy(), u, params, *sample(torch, lib, dev, u, params))
+
+
+@pytest.mark.parametrize("top_k", [33, 60, 113, 129, 197, 400, 1025])
+@pytest.mark.parametrize("M, V", [(40, 20011), (300, 5003), (2, 40000)])
+def test_top_k_of_many(torch, lib, M, V, top_k):
+    """A top-k beyond the numbers of parts of a row, of their groups and of their pairs."""
+    rng = np.random.default_rng([M, V, top_k])
+    dev = torch.from_numpy((rng.normal(size=(M, V)) * 3.0).astype(np.float32)).cuda()
+    for params in ((0.7, top_k, 1.0, 0.0), (1.0, top_k, 0.8, 0.01)):
+        u = rng.random(M, dtype=np.float32)
+        tokens, conf = sample(torch, lib, dev, u, params)
+        some = rng.choice(M, min(M, 12), replace=False)
+        check(dev.double().cpu().numpy()[some], u[some], params, tokens[some], conf[some])
