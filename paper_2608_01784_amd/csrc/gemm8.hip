@@ -484,19 +484,27 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
     w_cur[0] = w_next[0];
     w_cur[1] = w_next[1];
   };
-  // ---- prologue: the copies that the steps before the first would have issued
+  // ---- prologue: the first tile's scales (ahead of the copies: an access waits for all that were issued before
+  // it), then the copies that the steps before the first would have issued, in their order
   ready_a();
-  for (int q = 0; q < S::B_SLOTS - 1; ++q) {
+  Tile t = tile_at(0), next_t = t;
+  set_scales(t);
+  take_scales();
+#pragma unroll
+  for (int q = 0; q < SR; ++q) load_scale(q, s_row[q], t.rot);
+#pragma unroll
+  for (int v = 1 - S::B_SLOTS; v < 0; ++v) {
+    const int qa = v + S::A_SLOTS - 1, qb = v + S::B_SLOTS - 1;
+    if (qa >= 0) {
+      if (qa > 0 && a_k == nk) ready_a();
+      const int k = a_next();
+#pragma unroll
+      for (int j = 0; j < A_OPS; ++j) copy_a(j, a_ring + qa * S::A_BYTES, k);
+    }
     if (b_k == nk) ready_b();
     const int k = b_next();
 #pragma unroll
-    for (int j = 0; j < B_OPS; ++j) copy_b(j, b_ring + q * S::B_BYTES, k);
-  }
-  for (int q = 0; q < S::A_SLOTS - 1; ++q) {
-    if (q > 0 && a_k == nk) ready_a();
-    const int k = a_next();
-#pragma unroll
-    for (int j = 0; j < A_OPS; ++j) copy_a(j, a_ring + q * S::A_BYTES, k);
+    for (int j = 0; j < B_OPS; ++j) copy_b(j, b_ring + qb * S::B_BYTES, k);
   }
   // The K loop of one tile with NB active pair blocks (0: this wave only copies), group by group; at its
   // end s_cur holds the next tile's first group.
@@ -506,12 +514,6 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
   // are read while an earlier one multiplies, and a slice's last LATE units run after the next step's
   // barrier, while that slice's first fragments are read.  Units alternate between two fragment
   // registers; the late ones have their own.
-  Tile t = tile_at(0), next_t = t;
-  set_scales(t);
-  take_scales();
-#pragma unroll
-  for (int q = 0; q < SR; ++q) load_scale(q, s_row[q], t.rot);
-  wait_copies<0>();       // (not in the order that the steps count on)
   int s = 0;              // steps so far (the rings' slot counter)
   // One tile: K loop and epilogue, an instance per count of active blocks (with the accumulators inside,
   // which would be copied together from five places otherwise).
