@@ -4,8 +4,9 @@ The computation lives in ``libreflex.so`` (hand-written HIP kernels behind the C
 ABI declared in ``include/reflex.h``).  This package is its Python binding:
 ``_lib`` mirrors the C entry points one to one, ``layer`` runs the fused layer
 from torch tensors (experts in bf16 or in 8 bits), ``head`` predicts tokens and
-confidences of the masked positions, ``trajectory`` runs a whole decode.  Importing the package does not load the library; the first
-call does, and fails loudly if it has not been built.
+confidences of the masked positions, ``trajectory`` runs a whole decode.
+Importing the package does not load the library; the first call does, and fails
+loudly if it has not been built.
 """
 from ._lib import (  # noqa: F401
     ReflexError,

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
   // maxima of the pairs and of the groups of eight lanes (no elements: -inf)
   uint32_t group = f32_order_key(best);
   group = max(group, dpp_u32<kDppXor1>(group));
-  if (PAIRS && lane % 2 == 0) (a.pair + static_cast<size_t>(item) * (kWave / 2))[static_cast<uint32_t>(lane) / 2] = f32_from_order_key(group);
+  if (PAIRS && lane % 2 == 0) a.pair[static_cast<size_t>(item) * (kWave / 2) + lane / 2] = f32_from_order_key(group);
   group = max(group, dpp_u32<kDppXor2>(group));
   group = max(group, dpp_u32<kDppHalfMirror>(group));
   if (lane % 8 == 0) out->group[lane / 8] = f32_from_order_key(group);
@@ -488,7 +488,8 @@ RFX_DEVICE void row_flat(const SampleArgs& a, const RowParts& part, const double
 #pragma unroll
   for (int q = 0; q < SP_PARTS_LANE; ++q)
     if (kWave * q < a.parts)
-      most = max(most, (static_cast<uint64_t>(f32_order_key(part.top[q])) << 32) | (0x7fffffffu - static_cast<uint32_t>(part.first[q])));
+      most = max(most, (static_cast<uint64_t>(f32_order_key(part.top[q])) << 32) |
+                           (0x7fffffffu - static_cast<uint32_t>(part.first[q])));
   most = wave_max_u64(most);
   top = f32_from_order_key(static_cast<uint32_t>(most >> 32));
   first = static_cast<int>(0x7fffffffu - static_cast<uint32_t>(most));
