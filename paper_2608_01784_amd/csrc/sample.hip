@@ -53,6 +53,9 @@ constexpr int SP_SCAN = 8;                                // consecutive element
 static_assert(SP_BINS == 2 * SP_THREADS && SP_PARTS <= SP_THREADS, "two bins a thread");
 constexpr double SP_LOG2E = 1.4426950408889634074;
 constexpr float SP_NONE = -__builtin_huge_valf(), SP_LOWEST = -3.402823466e38f;
+// What stands in for a logit without weight where weights are summed.  Less any logit and times the least scale
+// (4.2e-39, the highest temperature's) it is below -4000, and finite times the largest (1e45).
+constexpr double SP_WEIGHTLESS = -1e42;
 
 #define SP_INLINE __attribute__((always_inline))
 
@@ -283,9 +286,9 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
     float z = 0.0f;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      const float l = fmaxf(v[k], SP_LOWEST);      // (NaN and -inf too: the weight of that is nothing)
       if (DRAWS) {
-        const double d = static_cast<double>(l) - static_cast<double>(ref);
+        // (NaN and -inf: far below every number that they may be relative to, at the highest temperature too)
+        const double d = fmax(static_cast<double>(v[k]), SP_WEIGHTLESS) - static_cast<double>(ref);
         const double y = fmax(fma(d, scale, kMagic), kMagic - 1020.0);      // (below 2^-1020: next to nothing)
         double p, t;
         pow2_parts(y, fma(d, scale, kMagic - y), table, p, t);
@@ -295,9 +298,15 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
           sum += k < n ? p * t : 0.0;
       }
       if (FLAT) {
-        const float w = __builtin_amdgcn_exp2f((l - ref) * static_cast<float>(SP_LOG2E));
+        const float w = __builtin_amdgcn_exp2f((v[k] - ref) * static_cast<float>(SP_LOG2E));
         z += WHOLE || k < n ? w : 0.0f;
       }
+    }
+    if (FLAT && z != z) {      // NaN among them, as -inf (told by the sum: no instruction an element)
+      z = 0.0f;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k)
+        z += (WHOLE || k < n) && v[k] == v[k] ? __builtin_amdgcn_exp2f((v[k] - ref) * static_cast<float>(SP_LOG2E)) : 0.0f;
     }
     if (FLAT) flat += static_cast<double>(z);
   });
