@@ -54,7 +54,7 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(
     const uint16_t* __restrict__ x, const int32_t* __restrict__ rows, const int32_t* __restrict__ n_rows,
     int x_rows, int M, int K, int groups, uint8_t* __restrict__ q, uint32_t* __restrict__ scale) {
   const int lane = threadIdx.x & 63;
-  const size_t item = static_cast<size_t>(blockIdx.x) * QR_WAVES + (threadIdx.x >> 6);
+  const size_t item = (static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * QR_WAVES + (threadIdx.x >> 6);
   const int row = static_cast<int>(item / groups), group = static_cast<int>(item % groups);
   const int used = n_rows == nullptr ? M : min(n_rows[0], M);
   if (row >= used) return;
@@ -110,8 +110,11 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_weight_kernel(const uint1
 int launch_quantize_rows(const uint16_t* x, const int32_t* rows, const int32_t* n_rows, int x_rows, int M, int K,
                          uint8_t* q, uint8_t* scale, hipStream_t s) {
   const int groups = f8_groups(K);
-  const size_t items = static_cast<size_t>(M) * groups;
-  hipLaunchKernelGGL(quantize_rows_kernel, dim3(static_cast<unsigned>((items + QR_WAVES - 1) / QR_WAVES)),
+  // (a dimension of a grid has less than 2^32 threads: 2^20 workgroups in x, the others in y)
+  const size_t blocks = (static_cast<size_t>(M) * groups + QR_WAVES - 1) / QR_WAVES, x_blocks = size_t(1) << 20;
+  const dim3 grid(static_cast<unsigned>(blocks < x_blocks ? blocks : x_blocks),
+                  static_cast<unsigned>((blocks + x_blocks - 1) / x_blocks));
+  hipLaunchKernelGGL(quantize_rows_kernel, grid,
                      dim3(QR_THREADS), 0, s, x, rows, n_rows, x_rows, M, K, groups, q,
                      reinterpret_cast<uint32_t*>(scale));
   return launch_status();
