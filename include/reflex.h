@@ -444,7 +444,8 @@ int reflex_quantize_fp8(const uint16_t* x, const int32_t* rows, const int32_t* n
 /*
  * bf16 weights of E experts (1: a plain matrix) to 8-bit weights.
  *  w [E, N, K] bf16;  q [E, N, K] codes;  scale [E, ceil(N / 128), 4 ceil(K / 512)]
- * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE; E up to REFLEX_MAX_EXPERTS).
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE; E up to REFLEX_MAX_EXPERTS, less than 2^24
+ *  blocks of 128 x 128).
  */
 int reflex_quantize_fp8_weight(const uint16_t* w, int E, int N, int K, uint8_t* q, uint8_t* scale,
                                void* stream);

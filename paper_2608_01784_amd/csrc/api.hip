@@ -726,7 +726,7 @@ int reflex_quantize_fp8_weight(const uint16_t* w, int E, int N, int K, uint8_t* 
   RFX_TRY(check_ptr(scale, 4));
   if (!valid_E(E) || !valid_T(N) || !valid_d(K)) return REFLEX_ERR_SHAPE;
   const long long blocks = static_cast<long long>(E) * ((N + F8_BLOCK - 1) / F8_BLOCK) * (K / F8_BLOCK);
-  if (blocks > INT32_MAX) return REFLEX_ERR_SHAPE;
+  if (blocks >= 1 << 24) return REFLEX_ERR_SHAPE;      // (2^38 numbers: more than a launch or the memory holds)
   if (N == 0) return REFLEX_OK;
   return launch_quantize_weight(w, E, N, K, q, scale, static_cast<hipStream_t>(stream));
 }
