@@ -49,6 +49,7 @@ constexpr int SP_LANE = 4, SP_SEG = SP_LANE * kWave;      // list entries of a l
 constexpr int SL_LANE = 16, SL_MOST = SL_LANE * kWave;    // a row's list: entries of a lane, of all
 constexpr int SL_LIST = 4 * SL_MOST;                      // the parts' shares of it are larger
 constexpr int SP_AROUND = 4;                              // bins listed on either side of a border's likely one
+constexpr int SP_ROWS = 1 << 16;                          // rows of a launch
 constexpr int SP_SCAN = 8;                                // consecutive elements of a thread in a scan
 static_assert(SP_BINS == 2 * SP_THREADS && SP_PARTS <= SP_THREADS, "two bins a thread");
 constexpr double SP_LOG2E = 1.4426950408889634074;
@@ -74,8 +75,8 @@ struct Listed {
 };
 
 struct SampleArgs {
-  const int32_t *rows, *n_rows;
-  int M, V, T, parts;
+  const int32_t *rows, *n_rows;      // rows: from row0 on
+  int M, V, T, parts, row0;          // M: rows of this launch; row0: the rows before them
   const float* u;
   double scale;          // log2(e) / temperature; 0: temperature 0
   double floor2;         // log2(min_p), -inf for none
@@ -88,6 +89,12 @@ struct SampleArgs {
   int32_t* listed;       // [M, parts]: the parts' numbers of listed elements, -1 for too many
   Listed* list;          // [M, SP_LIST]: parts' shares one after the other
 };
+
+// Rows of this launch that are in use, and row j's position.
+RFX_DEVICE int rows_used(const SampleArgs& a) {
+  return a.n_rows == nullptr ? a.M : min(max(a.n_rows[0], 0) - a.row0, a.M);
+}
+RFX_DEVICE int position_of(const SampleArgs& a, int j) { return a.rows == nullptr ? a.row0 + j : a.rows[j]; }
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 constexpr double kMagic = 0x1.8p46;      // its last place is 1 / 64
@@ -258,7 +265,7 @@ __global__ __launch_bounds__(SS_THREADS) void sample_sums_kernel(const E* __rest
   __syncthreads();
   const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + (tid >> 6));
   const int j = item / a.parts, part = item - j * a.parts;
-  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
+  if (j >= rows_used(a)) return;
   const Row<E> row(logits + static_cast<size_t>(j) * a.V, a.V, a.parts);
   const double scale = a.scale, step = fmax(scale, SP_LOG2E);
   float best = SP_NONE, ref = SP_LOWEST;
@@ -428,7 +435,7 @@ __global__ __launch_bounds__(SS_THREADS) void sample_list_kernel(const E* __rest
   __syncthreads();
   const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * SS_WAVES + (tid >> 6));
   const int j = item / a.parts, p = item - j * a.parts;      // (one row a workgroup: parts % SS_WAVES = 0)
-  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
+  if (j >= rows_used(a)) return;
   const Part* const part = a.part + static_cast<size_t>(j) * a.parts;
   if (tid < kWave) {
     float top;
@@ -541,8 +548,8 @@ __global__ __launch_bounds__(SS_THREADS) void sample_row_kernel(const E* __restr
     listed[q] = FILTERS && kWave * q + lane < parts ? a.listed[row_of + kWave * q + lane] : 0;
   if (tid < 64) table[tid] = pow2_entry(tid);
   __syncthreads();
-  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
-  const int pos = a.rows == nullptr ? j : a.rows[j];
+  if (j >= rows_used(a)) return;
+  const int pos = position_of(a, j);
   if (pos < 0 || pos >= a.T) return;
   const Row<E> row(logits + static_cast<size_t>(j) * V, V, parts);
   float top;
@@ -817,8 +824,8 @@ __global__ __launch_bounds__(SP_THREADS) void sample_flat_kernel(const E* __rest
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = blockIdx.x, V = a.V, parts = a.parts;
   const double scale = a.scale, least = a.floor2;
-  if (j >= (a.n_rows == nullptr ? a.M : min(a.n_rows[0], a.M))) return;
-  const int pos = a.rows == nullptr ? j : a.rows[j];
+  if (j >= rows_used(a)) return;
+  const int pos = position_of(a, j);
   if (pos < 0 || pos >= a.T) return;
   bool fits = true;
   int all = 0;
@@ -1351,13 +1358,16 @@ int parts_of(int M, int V) {
 
 static bool filters(const SampleArgs& a) { return a.top_k < a.V || a.top_p < 1.0 || a.floor2 > -1.0e300; }
 
-// The parts' records, the numbers of elements listed, the maxima of pairs, the lists.
+// Rows are taken SP_ROWS at a time, each with all launches (a launch has less than 2^32 threads, and the
+// workspace, some 33 KB a row, serves the next rows again).  Of those of a launch: the parts' records, the
+// numbers of elements listed, the maxima of pairs, the lists.
 static size_t part_bytes(int M, int V) { return align_up(sizeof(Part) * static_cast<size_t>(M) * parts_of(M, V)); }
 static size_t listed_bytes(int M, int V) { return align_up(sizeof(int32_t) * static_cast<size_t>(M) * parts_of(M, V)); }
 static size_t pair_bytes(int M, int V) {
   return align_up(sizeof(float) * (kWave / 2) * static_cast<size_t>(M) * parts_of(M, V));
 }
 size_t sample_ws_bytes(int M, int V) {
+  M = std::min(M, SP_ROWS);
   return part_bytes(M, V) + listed_bytes(M, V) + pair_bytes(M, V) + align_up(sizeof(Listed) * static_cast<size_t>(M) * SL_LIST);
 }
 
@@ -1385,18 +1395,26 @@ static int launch_sample_as(const E* logits, const SampleArgs& a, hipStream_t s)
 int launch_sample(const void* logits, int logits_type, const int32_t* rows, const int32_t* n_rows, int M, int V,
                   const float* u, const reflex_sample_params& p, int T, int32_t* tokens, float* conf, void* ws,
                   hipStream_t s) {
+  const int most = std::min(M, SP_ROWS);
   char* at[4] = {static_cast<char*>(ws)};
-  at[1] = at[0] + part_bytes(M, V);
-  at[2] = at[1] + listed_bytes(M, V);
-  at[3] = at[2] + pair_bytes(M, V);
-  const SampleArgs a{rows, n_rows, M, V, T, parts_of(M, V), u,
-                     p.temperature > 0.0f ? SP_LOG2E / static_cast<double>(p.temperature) : 0.0,
-                     p.min_p > 0.0f ? std::log2(static_cast<double>(p.min_p)) : -std::numeric_limits<double>::infinity(),
-                     p.top_k > 0 && p.top_k < V ? p.top_k : V, static_cast<double>(p.top_p), tokens, conf,
-                     reinterpret_cast<Part*>(at[0]), reinterpret_cast<float*>(at[2]), reinterpret_cast<int32_t*>(at[1]),
-                     reinterpret_cast<Listed*>(at[3])};
-  return logits_type == REFLEX_TYPE_F32 ? launch_sample_as(static_cast<const float*>(logits), a, s)
-                                        : launch_sample_as(static_cast<const uint16_t*>(logits), a, s);
+  at[1] = at[0] + part_bytes(most, V);
+  at[2] = at[1] + listed_bytes(most, V);
+  at[3] = at[2] + pair_bytes(most, V);
+  SampleArgs a{rows, n_rows, most, V, T, parts_of(most, V), 0, u,
+               p.temperature > 0.0f ? SP_LOG2E / static_cast<double>(p.temperature) : 0.0,
+               p.min_p > 0.0f ? std::log2(static_cast<double>(p.min_p)) : -std::numeric_limits<double>::infinity(),
+               p.top_k > 0 && p.top_k < V ? p.top_k : V, static_cast<double>(p.top_p), tokens, conf,
+               reinterpret_cast<Part*>(at[0]), reinterpret_cast<float*>(at[2]), reinterpret_cast<int32_t*>(at[1]),
+               reinterpret_cast<Listed*>(at[3])};
+  for (; a.row0 < M; a.row0 += most) {
+    a.M = std::min(most, M - a.row0);
+    a.rows = rows == nullptr ? nullptr : rows + a.row0;
+    const size_t first = static_cast<size_t>(a.row0) * V;
+    const int rc = logits_type == REFLEX_TYPE_F32 ? launch_sample_as(static_cast<const float*>(logits) + first, a, s)
+                                                  : launch_sample_as(static_cast<const uint16_t*>(logits) + first, a, s);
+    if (rc != REFLEX_OK) return rc;
+  }
+  return REFLEX_OK;
 }
 
 }  // namespace rfx
