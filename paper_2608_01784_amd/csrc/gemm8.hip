@@ -20,7 +20,7 @@
 // (measured: 1.4e-5 relative in the 2-norm, whatever K is), far inside the rounding to bf16 or e4m3
 // that follows, but not what an fp32 result promises.  PLAIN with fp32 results therefore widens the
 // codes to bf16 (one instruction for two, scale included; e4m3 numbers times powers of two are bf16
-// numbers) and multiplies on v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are
+// numbers, at the ends of the range by move_scales) and multiplies on v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are
 // fp32: a quarter of the rate, unnoticed where the weights' stream bounds the product.
 //
 // Data movement: operands go from global memory straight into LDS (16 bytes a lane) through rings
@@ -98,6 +98,46 @@ __device__ __forceinline__ bf16x8_t widen8(int lo, int hi, float scale) {
   const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
   const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Widened codes are bf16 numbers under scale bytes 3 .. 246.  Codes next to 448 under 247 are past bf16 (the
+// largest bf16 numbers round to 256 2^120), subnormal ones under 1 and 2 below its last place.  There a power of two
+// moves between the bytes of the wave's rows, x[i] a lane, and the byte w of the weights, which all of them share;
+// four slices' bytes at once.  (A row at the other end of the range then keeps its numbers to within 2^-133.)
+template <int MI>
+__device__ __forceinline__ void move_scales(uint32_t (&x)[MI], uint32_t& w) {
+  // below 16 or from 240 on: the upper four bits of a byte alike
+  auto maybe = [](uint32_t v) {
+    const uint32_t differ = (v ^ (v << 1)) & 0xe0e0e0e0u;
+    return ((differ - 0x01010101u) & ~differ & 0x80808080u) != 0;
+  };
+  bool some = maybe(w);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) some = some || maybe(x[i]);
+  if (!__any(some)) return;
+#pragma unroll 1
+  for (int at = 0; at < 32; at += 8) {
+    uint32_t least = 255, most = 0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      least = min(least, (x[i] >> at) & 0xffu);
+      most = max(most, (x[i] >> at) & 0xffu);
+    }
+    const bool high = __any(most > 246), near_high = __any(most > 244), low = __any(least < 3);
+    const uint32_t wb = (w >> at) & 0xffu;
+    int move = 0;
+    if (high)
+      move = -1;
+    else if (low)
+      move = near_high || wb < 5 ? 0 : 2;
+    else if (wb > 246)
+      move = near_high ? 0 : 1;
+    else if (wb < 3)
+      move = -2;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) x[i] += static_cast<uint32_t>(move) << at;
+    w -= static_cast<uint32_t>(move) << at;
+  }
 }
 
 __device__ __forceinline__ float silu_mul(float g, float u) {
@@ -661,6 +701,10 @@ __global__ __launch_bounds__(S::THREADS, 1) void fp8_gemm_kernel(Args8 a) {
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) sw[j] = __builtin_amdgcn_readlane(static_cast<int>(w_cur[j]), g);
+      if constexpr (WIDE) {
+        move_scales(sx, sw[0]);
+        sw[0] = __builtin_amdgcn_readfirstlane(static_cast<int>(sw[0]));
+      }
       if (done == 0 && !short_k) gather_a();
       g = last ? next_t.rot : (g + 1 < groups ? g + 1 : 0);
 #pragma unroll
@@ -854,7 +898,9 @@ __global__ __launch_bounds__(64 * W) void fp8_slim_kernel(Args8 a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (rows and columns past the last are the last one's again, and not stored)
   const uint8_t *x[MI], *w[NJ];
-  const uint32_t *xs[MI], *ws[NJ];
+  const uint32_t* xs[MI];
+  static_assert(F8_BLOCK % (32 * NJ) == 0, "a tile's columns in one block of weights");
+  const uint32_t* const ws = a.ss0 + static_cast<size_t>(n0 / F8_BLOCK) * groups;
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int r = min(row0 + 32 * i + lane % 32, rows - 1);
@@ -865,12 +911,11 @@ __global__ __launch_bounds__(64 * W) void fp8_slim_kernel(Args8 a) {
   for (int j = 0; j < NJ; ++j) {
     const int n = min(n0 + 32 * j + lane % 32, N - 1);
     w[j] = a.sw0 + static_cast<size_t>(n) * K + 32 * (lane / 32);
-    ws[j] = a.ss0 + static_cast<size_t>(min(n0 + 32 * j, N - 1) / F8_BLOCK) * groups;
   }
   // A slice: lane l has bytes 32 (l / 32) .. of each half of its rows' 128 (of both operands alike)
   struct Slice {
     i32x4_t x[MI][4], w[NJ][4];
-    uint32_t sx[MI], sw[NJ];
+    uint32_t sx[MI], sw;
   } slice[SLIM_AHEAD];
   auto load = [&](Slice& f, int k) {
     k = min(k, nk - 1);
@@ -886,8 +931,8 @@ __global__ __launch_bounds__(64 * W) void fp8_slim_kernel(Args8 a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         f.w[j][q] = *reinterpret_cast<const i32x4_t*>(w[j] + static_cast<size_t>(k) * G8_BK + 64 * (q / 2) + 16 * (q % 2));
-      f.sw[j] = ws[j][k >> 2];
     }
+    f.sw = ws[k >> 2];
   };
   f32x16_t acc[MI][NJ];
 #pragma unroll
@@ -896,13 +941,17 @@ __global__ __launch_bounds__(64 * W) void fp8_slim_kernel(Args8 a) {
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16_t{};
   auto multiply = [&](const Slice& f, int k) {
     const int shift = 8 * (k & 3);
+    uint32_t rows_scale[MI], weights_scale = f.sw;      // (the tile's columns lie in one block of 128)
+#pragma unroll
+    for (int i = 0; i < MI; ++i) rows_scale[i] = f.sx[i];
+    if constexpr (WIDE) move_scales(rows_scale, weights_scale);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          const uint32_t sx = (f.sx[i] >> shift) & 0xffu, sw = (f.sw[j] >> shift) & 0xffu;
+          const uint32_t sx = (rows_scale[i] >> shift) & 0xffu, sw = (weights_scale >> shift) & 0xffu;
           if constexpr (WIDE) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
