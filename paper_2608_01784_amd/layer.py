@@ -175,32 +175,61 @@ class ExpertWeights8:
                 _lib.want(where, scales + name, s, torch.uint8, _lib.fp8_weight_scale_shape(*shape))
                 if w.device != self.w_router.device or s.device != self.w_router.device:
                     raise ValueError(f"{where}: {codes + name} on {w.device}, the router on {self.w_router.device}")
+        _lib.want(where, "w_router", self.w_router, torch.float32, (E, d))
+        if self.router_bias is not None:
+            _lib.want(where, "router_bias", self.router_bias, torch.float32, (E,))
+            if self.router_bias.device != self.w_router.device:
+                raise ValueError(f"{where}: router_bias on {self.router_bias.device}, the router on "
+                                 f"{self.w_router.device}")
+
+    def tensors(self):
+        """All tensors, the 8-bit ones in the order of ``reflex_fp8_experts``, and their addresses."""
+        all_ = (self.w_gate, self.w_up, self.w_down, self.s_gate, self.s_up, self.s_down, self.ws_gate, self.ws_up,
+                self.ws_down, self.ss_gate, self.ss_up, self.ss_down, self.w_router, self.router_bias)
+        return all_, tuple(_lib.ptr(t) for t in all_)
 
 
 class MoELayer8(MoELayer):
     """MoELayer with the experts in 8 bits (``reflex_moe_forward_fp8``): hidden states come in and go
-    out in bf16, router, counts, TopK and combine are the same."""
+    out in bf16, router, counts, TopK and combine are the same.
+
+    A forward reads the tensors that ``w`` holds then, so weights can be replaced (by ones of the same
+    shapes) between forwards."""
 
     def __init__(self, T: int, d: int, weights: ExpertWeights8, *args, **kw):
         weights.check(d)
         super().__init__(T, d, weights, *args, **kw)
-        P, w = _lib.ptr, weights
-        self.experts = _lib.Fp8ExpertsC(P(w.w_gate), P(w.w_up), P(w.w_down), P(w.s_gate), P(w.s_up), P(w.s_down),
-                                        P(w.ws_gate), P(w.ws_up), P(w.ws_down), P(w.ss_gate), P(w.ss_up),
-                                        P(w.ss_down))
+        self._sizes = (weights.E, weights.f, weights.f_shared)
+        self._set_experts(*weights.tensors())
+
+    def _set_experts(self, tensors, addresses):
+        self._checked, self._addresses = tensors, addresses
+        self.experts = _lib.Fp8ExpertsC(*addresses[:12])
 
     def _workspace_bytes(self) -> int:
         w = self.w
         return _lib.reflex_workspace_fp8_size(self.T, w.E, self.d, w.f, w.f_shared, self.kcap)
 
-    def args(self, *args, **kw) -> _lib.MoeArgsC:
-        a = super().args(*args, **kw)
+    def _check_weights(self):
+        w, where = self.w, "MoELayer8"
+        tensors, addresses = w.tensors()
+        # replaced: other tensors, or the same ones with other memory
+        if addresses != self._addresses or any(a is not b for a, b in zip(tensors, self._checked)):
+            w.check(self.d)
+            if (w.E, w.f, w.f_shared) != self._sizes:
+                raise ValueError(f"{where}: weights of (E, f, f_shared) = {(w.E, w.f, w.f_shared)} in a layer made "
+                                 f"for {self._sizes}")
+            self._set_experts(tensors, addresses)
+
+    def args(self, h, state=None, k_in=None, residual_a=None, residual_b=None, out=None) -> _lib.MoeArgsC:
+        self._check_weights()
+        a = super().args(h, state, k_in, residual_a, residual_b, out)
         a.w_gate = a.w_up = a.w_down = a.ws_gate = a.ws_up = a.ws_down = None      # (bf16 weights: not read)
         return a
 
     def forward(self, h, state=None, k_in=None, residual_a=None, residual_b=None, out=None,
                 stream=None) -> torch.Tensor:
+        args = self.args(h, state, k_in, residual_a, residual_b, out)
         if self.T > 0:      # (empty tensors have no address)
-            args = self.args(h, state, k_in, residual_a, residual_b, out)
             _lib.reflex_moe_forward_fp8(args, self.experts, self.ws, stream)
         return self.out if out is None else out

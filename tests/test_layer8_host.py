@@ -1,0 +1,71 @@
+"""MoELayer8 reads the weights that it holds at the time of a forward (no GPU needed)."""
+import os
+
+import pytest
+
+_lib = pytest.importorskip("paper_2608_01784_amd._lib")
+torch = pytest.importorskip("torch")
+
+from test_abi_fp8 import bf, u8, weights8  # noqa: E402
+
+T, d = 16, 256
+
+
+class P:
+    k_base, delta_role, delta_cur, k_min, k_max = 2, 1, 1, 1, 2
+    q, theta, w_cf, v_ref, tau = 0.5, 0.9, 0.5, 0.1, 0.1
+
+
+@pytest.fixture
+def layer():
+    from paper_2608_01784_amd.layer import MoELayer8
+    if not os.path.exists(_lib.LIB_PATH):
+        pytest.fail("libreflex.so is not built (python -m paper_2608_01784_amd.build)")
+    return MoELayer8(T, d, weights8(fs=128), P(), uniform_k=2, device="cpu")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The structs of the calls that a forward would make."""
+    made = []
+    monkeypatch.setattr(_lib, "reflex_moe_forward_fp8", lambda args, experts, ws, stream=None: made.append((args, experts)))
+    return made
+
+
+NAMES = [n for n, _ in _lib.Fp8ExpertsC._fields_]
+
+
+def test_forward_reads_the_weights_it_holds(layer, calls):
+    layer.forward(bf(T, d))
+    for name in NAMES:
+        setattr(layer.w, name, torch.zeros_like(getattr(layer.w, name)))
+        layer.forward(bf(T, d))
+        got = [getattr(calls[-1][1], n) for n in NAMES]
+        assert got == [getattr(layer.w, n).data_ptr() for n in NAMES], name
+    layer.w.w_router = torch.zeros(2, d)
+    layer.forward(bf(T, d))
+    assert calls[-1][0].w_router == layer.w.w_router.data_ptr() and calls[-1][0].w_gate is None
+    layer.w.w_up.data = torch.zeros_like(layer.w.w_up)      # (the same tensor with other memory)
+    layer.forward(bf(T, d))
+    assert calls[-1][1].w_up == layer.w.w_up.data_ptr()
+    layer.w = weights8(fs=128)      # (all of them)
+    layer.forward(bf(T, d))
+    assert [getattr(calls[-1][1], n) for n in NAMES] == [getattr(layer.w, n).data_ptr() for n in NAMES]
+
+
+@pytest.mark.parametrize("name, bad", [("w_gate", u8(2, 128, 384)), ("ws_down", None), ("s_up", u8(2, 2, 4)),
+                                       ("w_router", torch.zeros(2, 128)), ("router_bias", torch.zeros(3)),
+                                       ("w_down", bf(2, 256, 128))])
+def test_replaced_weights_are_checked(layer, calls, name, bad):
+    setattr(layer.w, name, bad)
+    with pytest.raises((ValueError, TypeError)):
+        layer.forward(bf(T, d))
+    assert not calls
+
+
+def test_weights_of_other_sizes_are_refused(layer, calls):
+    for w in (weights8(E=3, fs=128), weights8(f=256, fs=128), weights8()):
+        layer.w = w
+        with pytest.raises(ValueError, match="made for"):
+            layer.forward(bf(T, d))
+    assert not calls
