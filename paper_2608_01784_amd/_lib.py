@@ -467,9 +467,9 @@ def reflex_workspace_fp8_size(T, E, d, f, f_shared, k_max) -> int:
 
 
 def reflex_moe_forward_fp8(args: MoeArgsC, experts: Fp8ExpertsC, ws, stream=None):
-    _check(lib().reflex_moe_forward_fp8(ctypes.byref(args), ctypes.byref(experts), ptr(ws),
-                                        ws.numel() * ws.element_size(), stream_handle(stream)),
-           "reflex_moe_forward_fp8")
+    """The structs hold addresses: whoever fills them checks the tensors behind (``layer.MoELayer8`` does)."""
+    _launch("reflex_moe_forward_fp8", (ws,),
+            (ctypes.byref(args), ctypes.byref(experts), address(ws), ws.numel() * ws.element_size()), stream)
 
 
 def reflex_sample_workspace_size(M, V) -> int:

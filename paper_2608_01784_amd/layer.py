@@ -194,11 +194,16 @@ class MoELayer8(MoELayer):
     out in bf16, router, counts, TopK and combine are the same.
 
     A forward reads the tensors that ``w`` holds then, so weights can be replaced (by ones of the same
-    shapes) between forwards."""
+    shapes) between forwards.  It checks types, shapes, density and device of all tensors (the C call sees
+    addresses alone) and runs on the layer's device, that of the weights."""
 
-    def __init__(self, T: int, d: int, weights: ExpertWeights8, *args, **kw):
+    def __init__(self, T: int, d: int, weights: ExpertWeights8, params, uniform_k: int = 0, norm_topk: int = 1,
+                 k_rule: int = 0, k_threshold: float = 0.0, device=None):
         weights.check(d)
-        super().__init__(T, d, weights, *args, **kw)
+        at = weights.w_router.device
+        if device is not None and torch.empty(0, device=device).device != at:
+            raise ValueError(f"MoELayer8: device {device}, but weights on {at}")
+        super().__init__(T, d, weights, params, uniform_k, norm_topk, k_rule, k_threshold, at)
         self._sizes = (weights.E, weights.f, weights.f_shared)
         self._set_experts(*weights.tensors())
 
@@ -210,8 +215,8 @@ class MoELayer8(MoELayer):
         w = self.w
         return _lib.reflex_workspace_fp8_size(self.T, w.E, self.d, w.f, w.f_shared, self.kcap)
 
-    def _check_weights(self):
-        w, where = self.w, "MoELayer8"
+    def _check(self, h, state, k_in, residual_a, residual_b, out):
+        w, where, T = self.w, "MoELayer8", self.T
         tensors, addresses = w.tensors()
         # replaced: other tensors, or the same ones with other memory
         if addresses != self._addresses or any(a is not b for a, b in zip(tensors, self._checked)):
@@ -220,9 +225,31 @@ class MoELayer8(MoELayer):
                 raise ValueError(f"{where}: weights of (E, f, f_shared) = {(w.E, w.f, w.f_shared)} in a layer made "
                                  f"for {self._sizes}")
             self._set_experts(tensors, addresses)
+        rows = [("h", h, torch.bfloat16, (T, self.d))]
+        for name, t in (("residual_a", residual_a), ("residual_b", residual_b), ("out", out)):
+            if t is not None:
+                rows.append((name, t, torch.bfloat16, (T, self.d)))
+        if k_in is not None:
+            rows.append(("k_in", k_in, torch.int32, (T,)))
+        if state is not None:
+            B = state.active_block.shape[0]
+            rows += [("block_idx", state.block_idx, torch.int32, (T,)),
+                     ("masked", state.masked, (torch.uint8, torch.bool), (T,)),
+                     ("hist_len", state.hist_len, torch.int8, (T,)),
+                     ("conf_prev1", state.conf_prev1, torch.float32, (T,)),
+                     ("conf_prev2", state.conf_prev2, torch.float32, (T,)),
+                     ("seq_offsets", state.seq_offsets, torch.int32, (B + 1,)),
+                     ("active_block", state.active_block, torch.int32, (B,))]
+        at = self.ws.get_device()
+        if w.w_router.get_device() != at:
+            raise ValueError(f"{where}: weights on {w.w_router.device}, the layer on {self.ws.device}")
+        for name, t, dtype, shape in rows:
+            _lib.want(where, name, t, dtype, shape)
+            if t.get_device() != at:
+                raise ValueError(f"{where}: {name} on {t.device}, the layer on {self.ws.device}")
 
     def args(self, h, state=None, k_in=None, residual_a=None, residual_b=None, out=None) -> _lib.MoeArgsC:
-        self._check_weights()
+        self._check(h, state, k_in, residual_a, residual_b, out)
         a = super().args(h, state, k_in, residual_a, residual_b, out)
         a.w_gate = a.w_up = a.w_down = a.ws_gate = a.ws_up = a.ws_down = None      # (bf16 weights: not read)
         return a

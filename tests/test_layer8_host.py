@@ -1,4 +1,6 @@
-"""MoELayer8 reads the weights that it holds at the time of a forward (no GPU needed)."""
+"""MoELayer8 reads the weights it is given at the time of a forward, and refuses tensors that the C call,
+which sees addresses alone, would read past their end or as another type (no GPU needed)."""
+import dataclasses
 import os
 
 import pytest
@@ -6,7 +8,7 @@ import pytest
 _lib = pytest.importorskip("paper_2608_01784_amd._lib")
 torch = pytest.importorskip("torch")
 
-from test_abi_fp8 import bf, u8, weights8  # noqa: E402
+from test_abi_fp8 import bf, i32, u8, weights8  # noqa: E402
 
 T, d = 16, 256
 
@@ -22,6 +24,12 @@ def layer():
     if not os.path.exists(_lib.LIB_PATH):
         pytest.fail("libreflex.so is not built (python -m paper_2608_01784_amd.build)")
     return MoELayer8(T, d, weights8(fs=128), P(), uniform_k=2, device="cpu")
+
+
+def state(**kw):
+    from paper_2608_01784_amd.layer import TokenState
+    s = TokenState(i32(T), u8(T), torch.zeros(T, dtype=torch.int8), torch.zeros(T), torch.zeros(T), i32(2), i32(1))
+    return dataclasses.replace(s, **kw)
 
 
 @pytest.fixture
@@ -69,3 +77,31 @@ def test_weights_of_other_sizes_are_refused(layer, calls):
         with pytest.raises(ValueError, match="made for"):
             layer.forward(bf(T, d))
     assert not calls
+
+
+@pytest.mark.parametrize("name, bad", [
+    ("h", torch.zeros(T, d)), ("h", bf(T - 1, d)), ("h", bf(T, 2 * d)[:, ::2]), ("h", bf(T, 128)),
+    ("residual_a", torch.zeros(T, d)), ("residual_b", bf(T + 1, d)), ("out", bf(d, T).t()),
+    ("out", torch.zeros(T, d, dtype=torch.float16)), ("k_in", torch.zeros(T, dtype=torch.int64)), ("k_in", i32(T - 1)),
+    ("state", state(block_idx=i32(T - 1))), ("state", state(masked=i32(T))), ("state", state(hist_len=u8(T))),
+    ("state", state(conf_prev1=torch.zeros(T, dtype=torch.float64))), ("state", state(conf_prev2=torch.zeros(1))),
+    ("state", state(seq_offsets=i32(1))), ("state", state(active_block=torch.zeros(1)))])
+def test_operands_are_checked(layer, calls, name, bad):
+    good = dict(h=bf(T, d), state=state(), k_in=i32(T), residual_a=bf(T, d), residual_b=bf(T, d), out=bf(T, d))
+    assert layer.forward(**good) is good["out"] and len(calls) == 1
+    with pytest.raises((ValueError, TypeError), match=None if name == "state" else name):
+        layer.forward(**dict(good, **{name: bad}))
+    assert len(calls) == 1
+
+
+def test_host_memory_is_refused(layer):
+    with pytest.raises(ValueError, match="device memory"):
+        layer.forward(bf(T, d))
+
+
+def test_layer_is_on_its_weights_device():
+    from paper_2608_01784_amd.layer import MoELayer8
+    lay = MoELayer8(T, d, weights8(), P(), uniform_k=2)
+    assert lay.ws.device == lay.out.device == torch.device("cpu")
+    with pytest.raises(ValueError, match="device"):
+        MoELayer8(T, d, weights8(), P(), uniform_k=2, device="meta")
