@@ -259,4 +259,6 @@ class MoELayer8(MoELayer):
         args = self.args(h, state, k_in, residual_a, residual_b, out)
         if self.T > 0:      # (empty tensors have no address)
             _lib.reflex_moe_forward_fp8(args, self.experts, self.ws, stream)
+        else:               # (the call enqueues nothing)
+            self.pairs.zero_()
         return self.out if out is None else out

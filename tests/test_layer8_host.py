@@ -105,3 +105,11 @@ def test_layer_is_on_its_weights_device():
     assert lay.ws.device == lay.out.device == torch.device("cpu")
     with pytest.raises(ValueError, match="device"):
         MoELayer8(T, d, weights8(), P(), uniform_k=2, device="meta")
+
+
+def test_layer_without_tokens_has_no_pairs(calls):
+    from paper_2608_01784_amd.layer import MoELayer8
+    lay = MoELayer8(0, d, weights8(), P(), uniform_k=2)
+    lay.pairs.fill_(7)
+    lay.forward(bf(0, d))
+    assert int(lay.pairs) == 0 and not calls
