@@ -329,6 +329,15 @@ def want(where, name, t, dtypes, shape):
         raise ValueError(f"{where}: {name} is not contiguous")
 
 
+def space(where, ws):
+    """Address and bytes of a workspace (None: nothing)."""
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():      # (its elements would be counted, not the memory behind them)
+        raise ValueError(f"{where}: ws is not contiguous")
+    return address(ws), ws.numel() * ws.element_size()
+
+
 def _launch(where, tensors, args, stream):
     """Call entry point `where` with args and the stream, on the tensors' device."""
     import torch
@@ -383,8 +392,7 @@ def reflex_select_rows(masked, rows, n_rows, ws=None, stream=None):
     want(where, "rows", rows, torch.int32, (T,))
     want(where, "n_rows", n_rows, torch.int32, (1,))
     _launch(where, (masked, rows, n_rows, ws),
-            (address(masked), T, address(rows), address(n_rows), address(ws),
-             0 if ws is None else ws.numel() * ws.element_size()), stream)
+            (address(masked), T, address(rows), address(n_rows), *space(where, ws)), stream)
 
 
 def reflex_quantize_fp8(x, q, scale, rows=None, n_rows=None, stream=None):
@@ -459,7 +467,7 @@ def reflex_grouped_swiglu_fp8(h, h_scale, sorted_token, expert_offsets, w_gate, 
                     s_down, y_sorted, ws),
             (address(h), address(h_scale), address(sorted_token), address(expert_offsets), address(w_gate), address(w_up),
              address(w_down), address(s_gate), address(s_up), address(s_down), T, E, d, f, cap, address(y_sorted),
-             address(ws), ws.numel() * ws.element_size()), stream)
+             *space(where, ws)), stream)
 
 
 def reflex_workspace_fp8_size(T, E, d, f, f_shared, k_max) -> int:
@@ -468,8 +476,8 @@ def reflex_workspace_fp8_size(T, E, d, f, f_shared, k_max) -> int:
 
 def reflex_moe_forward_fp8(args: MoeArgsC, experts: Fp8ExpertsC, ws, stream=None):
     """The structs hold addresses: whoever fills them checks the tensors behind (``layer.MoELayer8`` does)."""
-    _launch("reflex_moe_forward_fp8", (ws,),
-            (ctypes.byref(args), ctypes.byref(experts), address(ws), ws.numel() * ws.element_size()), stream)
+    where = "reflex_moe_forward_fp8"
+    _launch(where, (ws,), (ctypes.byref(args), ctypes.byref(experts), *space(where, ws)), stream)
 
 
 def reflex_sample_workspace_size(M, V) -> int:
@@ -495,5 +503,5 @@ def reflex_sample_tokens(logits, u, params: SampleParamsC, tokens, conf=None, ro
         want(where, "n_rows", n_rows, torch.int32, (1,))
     _launch(where, (logits, u, tokens, conf, rows, n_rows, ws),
             (address(logits), TYPE_F32 if logits.dtype == torch.float32 else TYPE_BF16, address(rows),
-             address(n_rows), M, V, address(u), ctypes.byref(params), T, address(tokens), address(conf), address(ws),
-             0 if ws is None else ws.numel() * ws.element_size()), stream)
+             address(n_rows), M, V, address(u), ctypes.byref(params), T, address(tokens), address(conf),
+             *space(where, ws)), stream)
