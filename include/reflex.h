@@ -502,8 +502,9 @@ int reflex_moe_forward_fp8(const reflex_moe_args* args, const reflex_fp8_experts
  * The token a forward predicts at each position and its confidence c^t (Section 3.1), as
  * reflex_advance_state takes it, from rows of logits and given uniform numbers.
  * Row j of the logits is position i = rows[j] (rows NULL: i = j), j < n_rows[0] (n_rows
- * NULL: M); positions outside [0, T) are skipped, those of no row are left as they were,
- * one of several rows has the result of any of them.
+ * NULL: M); positions outside [0, T) are skipped, those of no row are left as they were.
+ * Where a position is listed twice, tokens[i] and conf[i] are each of one of its rows, not
+ * always of the same one.
  *   weight of token v:  w_v = exp((l_v - max l) / temperature), in fp64
  *   kept tokens, in the order (logit descending, index ascending, -0.0 == +0.0): the first
  *     top_k; of those the shortest prefix whose weights sum to at least top_p of theirs;
