@@ -18,10 +18,12 @@
 //
 // Precision: the f8f6f4 MFMA adds its 64 products with about 17 bits below the largest of them
 // (measured: 1.4e-5 relative in the 2-norm, whatever K is), far inside the rounding to bf16 or e4m3
-// that follows, but not what an fp32 result promises.  PLAIN with fp32 results therefore widens the
-// codes to bf16 (one instruction for two, scale included; e4m3 numbers times powers of two are bf16
-// numbers, at the ends of the range by move_scales) and multiplies on v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are
-// fp32: a quarter of the rate, unnoticed where the weights' stream bounds the product.
+// that follows (but a code of the activation next to a border may be the other one: experts are 1.8e-3 to
+// 2.1e-3 from 64 bits where fp32 sums leave 1.7e-3), and not what an fp32 result promises.  PLAIN with fp32
+// results therefore widens the codes to bf16 (one instruction for two, scale included; e4m3 numbers times
+// powers of two are bf16 numbers, at the ends of the range with move_scales) and multiplies on
+// v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are fp32: a quarter of the rate,
+// unnoticed where the weights' stream bounds the product.
 //
 // Data movement: operands go from global memory straight into LDS (16 bytes a lane) through rings
 // of slices.  LDS rows are 128 bytes (8 chunks of 16) with chunk c of row r in slot

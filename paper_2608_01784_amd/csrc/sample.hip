@@ -41,8 +41,8 @@
 namespace rfx {
 namespace {
 
-constexpr int SS_THREADS = 256, SS_WAVES = SS_THREADS / kWave;      // first launch
-constexpr int SP_THREADS = 1024, SP_WAVES = SP_THREADS / kWave;     // second launch
+constexpr int SS_THREADS = 256, SS_WAVES = SS_THREADS / kWave;      // launches 1 to 3
+constexpr int SP_THREADS = 1024, SP_WAVES = SP_THREADS / kWave;     // launch 4
 constexpr int SP_PARTS = 256;                                       // most parts of a row
 constexpr int SP_BIN_BITS = 11, SP_BINS = 1 << SP_BIN_BITS;
 constexpr int SP_LANE = 4, SP_SEG = SP_LANE * kWave;      // list entries of a lane and of a wave
@@ -1359,7 +1359,7 @@ int parts_of(int M, int V) {
 static bool filters(const SampleArgs& a) { return a.top_k < a.V || a.top_p < 1.0 || a.floor2 > -1.0e300; }
 
 // Rows are taken SP_ROWS at a time, each with all launches (a launch has less than 2^32 threads, and the
-// workspace, some 33 KB a row, serves the next rows again).  Of those of a launch: the parts' records, the
+// workspace, 33 to 81 KB a row, serves the next rows again).  Of those of a launch: the parts' records, the
 // numbers of elements listed, the maxima of pairs, the lists.
 static size_t part_bytes(int M, int V) { return align_up(sizeof(Part) * static_cast<size_t>(M) * parts_of(M, V)); }
 static size_t listed_bytes(int M, int V) { return align_up(sizeof(int32_t) * static_cast<size_t>(M) * parts_of(M, V)); }
