@@ -24,12 +24,14 @@
 //     keys of one bin, in passes over the row (in the memory-side cache by then) until what is left
 //     fits a list in LDS.  (Fixed-point weights: the sums do not depend on the order of the atomics.)  The
 //     draw goes over the row's sixteenths and a scan of one.
-// Everything is inlined and in registers: no stack.
+// Everything is inlined and in registers: no stack.  (Keep it so, ScratchSize 0 in the build's resource report: a
+// form that used one gave a wrong token and a GPU fault whose cause was never shown.)
 //
-// Measured, us (bf16 logits, temperature 1): 1024 rows of 100003 without filters 104 (launch 1: 90, bound by its
-// 32 vector instructions an element, where reading the logits takes 34), top-k 50 169, min-p 0.02 208, top-p 0.9 400 (launch 4:
-// 270 for 665 flat rows, 75 a row, bound by 50 vector instructions an element on the row's own CU); 32 rows of
-// 131072 17, 28, 65 and 106, with all filters (temperature 0.7, top-k 50, top-p 0.9, min-p 0.02) 35, of which launch 3
+// Measured, us (bf16 logits, temperature 1): 1024 rows of 100003 without filters 95 (launch 1: 86, bound by its
+// 29 vector instructions an element, where reading the logits takes 34; 114 at another temperature, whose
+// confidences want sums of their own; greedy 47), top-k 50 166, min-p 0.02 202, top-p 0.9 394 (launch 4:
+// 262 for the flat rows, 75 a row, bound by 50 vector instructions an element on the row's own CU); 32 rows of
+// 131072 16, 28, 65 and 106, with all filters (temperature 0.7, top-k 50, top-p 0.9, min-p 0.02) 34, of which launch 3
 // takes 17: one wave's chain of loads and the bit by bit search for two borders; one row of 32000 10, two launches.
 #include <algorithm>
 #include <cmath>

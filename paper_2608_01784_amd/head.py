@@ -23,7 +23,7 @@ class TokenHead:
     ``quantize_weight`` gives them.  tokens int32 [T] and conf float32 [T] hold the last
     prediction at every position: -1 and 0 until there is one, and from the forward that
     commits a position on what that forward predicted.  logits: [T, V], the masked positions'
-    rows in front."""
+    rows in front (room for all of them: 4.3 GB for 8192 positions of 131072 tokens in fp32)."""
 
     def __init__(self, T: int, weight, temperature: float = 0.0, top_k: int = 0, top_p: float = 1.0,
                  min_p: float = 0.0, logits_dtype=torch.float32):
