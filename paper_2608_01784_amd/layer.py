@@ -225,28 +225,34 @@ class MoELayer8(MoELayer):
                 raise ValueError(f"{where}: weights of (E, f, f_shared) = {(w.E, w.f, w.f_shared)} in a layer made "
                                  f"for {self._sizes}")
             self._set_experts(tensors, addresses)
-        rows = [("h", h, torch.bfloat16, (T, self.d))]
-        for name, t in (("residual_a", residual_a), ("residual_b", residual_b), ("out", out)):
-            if t is not None:
-                rows.append((name, t, torch.bfloat16, (T, self.d)))
-        if k_in is not None:
-            rows.append(("k_in", k_in, torch.int32, (T,)))
-        if state is not None:
-            B = state.active_block.shape[0]
-            rows += [("block_idx", state.block_idx, torch.int32, (T,)),
-                     ("masked", state.masked, (torch.uint8, torch.bool), (T,)),
-                     ("hist_len", state.hist_len, torch.int8, (T,)),
-                     ("conf_prev1", state.conf_prev1, torch.float32, (T,)),
-                     ("conf_prev2", state.conf_prev2, torch.float32, (T,)),
-                     ("seq_offsets", state.seq_offsets, torch.int32, (B + 1,)),
-                     ("active_block", state.active_block, torch.int32, (B,))]
         at = self.ws.get_device()
         if w.w_router.get_device() != at:
             raise ValueError(f"{where}: weights on {w.w_router.device}, the layer on {self.ws.device}")
-        for name, t, dtype, shape in rows:
-            _lib.want(where, name, t, dtype, shape)
+
+        def check(name, t, types, n, width=None):      # (positions may be spread over several dimensions)
+            if t.dtype not in types:
+                raise TypeError(f"{where}: {name} has element type {t.dtype}, not {types}")
+            if t.numel() != n or (width is not None and t.shape[-1] != width):
+                of = "" if width is None else f" in rows of {width}"
+                raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {n} elements{of}")
+            if not t.is_contiguous():
+                raise ValueError(f"{where}: {name} is not contiguous")
             if t.get_device() != at:
                 raise ValueError(f"{where}: {name} on {t.device}, the layer on {self.ws.device}")
+        for name, t in (("h", h), ("residual_a", residual_a), ("residual_b", residual_b), ("out", out)):
+            if t is not None or name == "h":
+                check(name, t, (torch.bfloat16,), T * self.d, self.d)
+        if k_in is not None:
+            check("k_in", k_in, (torch.int32,), T)
+        if state is not None:
+            B = state.active_block.shape[0]
+            check("active_block", state.active_block, (torch.int32,), B)
+            check("seq_offsets", state.seq_offsets, (torch.int32,), B + 1)
+            check("block_idx", state.block_idx, (torch.int32,), T)
+            check("masked", state.masked, (torch.uint8, torch.int8, torch.bool), T)
+            check("hist_len", state.hist_len, (torch.int8, torch.uint8), T)
+            check("conf_prev1", state.conf_prev1, (torch.float32,), T)
+            check("conf_prev2", state.conf_prev2, (torch.float32,), T)
 
     def args(self, h, state=None, k_in=None, residual_a=None, residual_b=None, out=None) -> _lib.MoeArgsC:
         self._check(h, state, k_in, residual_a, residual_b, out)

@@ -83,7 +83,7 @@ def test_weights_of_other_sizes_are_refused(layer, calls):
     ("h", torch.zeros(T, d)), ("h", bf(T - 1, d)), ("h", bf(T, 2 * d)[:, ::2]), ("h", bf(T, 128)),
     ("residual_a", torch.zeros(T, d)), ("residual_b", bf(T + 1, d)), ("out", bf(d, T).t()),
     ("out", torch.zeros(T, d, dtype=torch.float16)), ("k_in", torch.zeros(T, dtype=torch.int64)), ("k_in", i32(T - 1)),
-    ("state", state(block_idx=i32(T - 1))), ("state", state(masked=i32(T))), ("state", state(hist_len=u8(T))),
+    ("state", state(block_idx=i32(T - 1))), ("state", state(masked=i32(T))), ("state", state(hist_len=i32(T))),
     ("state", state(conf_prev1=torch.zeros(T, dtype=torch.float64))), ("state", state(conf_prev2=torch.zeros(1))),
     ("state", state(seq_offsets=i32(1))), ("state", state(active_block=torch.zeros(1)))])
 def test_operands_are_checked(layer, calls, name, bad):
@@ -92,6 +92,15 @@ def test_operands_are_checked(layer, calls, name, bad):
     with pytest.raises((ValueError, TypeError), match=None if name == "state" else name):
         layer.forward(**dict(good, **{name: bad}))
     assert len(calls) == 1
+
+
+def test_positions_in_several_dimensions(layer, calls):
+    """(sequences, positions, d): what counts is the memory."""
+    s = state(block_idx=i32(4, 4), masked=torch.zeros(T, dtype=torch.bool), conf_prev1=torch.zeros(4, 4))
+    layer.forward(bf(4, 4, d), s, residual_a=bf(2, 8, d), out=bf(1, T, d))
+    assert len(calls) == 1
+    with pytest.raises(ValueError, match="rows of"):
+        layer.forward(bf(d, T))
 
 
 def test_host_memory_is_refused(layer):
