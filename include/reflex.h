@@ -507,6 +507,145 @@ size_t reflex_workspace_fp8_size(int T, int E, int d, int f, int f_shared, int k
 int reflex_moe_forward_fp8(const reflex_moe_args* args, const reflex_fp8_experts* experts, void* ws,
                            size_t ws_bytes, void* stream);
 
+/* ---- 8-bit integer products ------------------------------------------------------------
+ * Matrices of 8-bit integers (-127 .. 127) with one fp32 scale for each row: a token of the
+ * input, an output channel of the weights.  a = the row's largest magnitude (2^-100 at least):
+ * the scale is a / 127, a code the number times (127 / a), rounded to nearest with ties to even
+ * (quotients and product rounded to fp32 first).  A row that holds a number which is not finite
+ * has codes 0 and the scale NaN: whatever is computed from it is NaN, and nothing else is.
+ *
+ *  rows     codes [M, K] row-major, scale [M] fp32
+ *  weights  codes [N, K] row-major, scale [N] fp32 (experts one after the other)
+ * Codes of -128 are multiplied as such.  K is a multiple of 128 and at most REFLEX_MAX_DIM; M and
+ * N are any.  Codes must be 16-byte aligned, scales 4-byte aligned.
+ *
+ * bf16 rows to 8-bit rows; x, rows, n_rows, x_rows as in reflex_quantize_fp8.
+ *  q [M, K] codes;  scale [M]
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE); rows NULL with x_rows < M.
+ */
+int reflex_quantize_int8(const uint16_t* x, const int32_t* rows, const int32_t* n_rows, int x_rows,
+                         int M, int K, int8_t* q, float* scale, void* stream);
+
+/*
+ * bf16 weights of E experts (1: a plain matrix) to 8-bit weights.
+ *  w [E, N, K] bf16;  q [E, N, K] codes;  scale [E, N]
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE; E up to REFLEX_MAX_EXPERTS, E N less than 2^31).
+ */
+int reflex_quantize_int8_weight(const uint16_t* w, int E, int N, int K, int8_t* q, float* scale,
+                                void* stream);
+
+/*
+ * out[i, n] = (sum_k x[i, k] w[n, k]) (x_scale[i] w_scale[n]): the sum of the codes' products is
+ * exact, on the matrix cores; it, the product of the scales and the result are rounded to fp32
+ * (off by at most 3 2^-24 of itself), for bf16 results then to bf16.  Rows from n_rows[0] on
+ * (n_rows NULL: M) are left as they were.
+ *  x [M, K], x_scale [M];  w [N, K], w_scale [N];  out [M, N] dense (16-byte aligned), out_type
+ *  REFLEX_TYPE_*
+ * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE); unknown out_type (REFLEX_ERR_PARAM).
+ */
+int reflex_matmul_int8(const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale,
+                       const int32_t* n_rows, int M, int N, int K, int out_type, void* out,
+                       void* stream);
+
+/*
+ * reflex_grouped_swiglu on 8-bit integers.  For row j of expert e, x the row sorted_token[j] of
+ * h:  g = W_gate[e] x and u = W_up[e] x as fp32 results of reflex_matmul_int8, SiLU(g) * u rounded
+ * to bf16, that row rounded to 8 bits as reflex_quantize_int8 does, y_sorted[j] = W_down[e] of it
+ * as a bf16 result of reflex_matmul_int8.  SiLU is within (|g| + 4) 2^-22 of itself; a value that
+ * this or a rounding takes across a border between two codes has the other one, a step away.
+ *  h [T, d], h_scale [T];  w_gate, w_up [E, f, d], w_down [E, d, f] with s_gate, s_up [E, f],
+ *  s_down [E, d];  sorted_token, expert_offsets, pair_capacity, y_sorted as in
+ *  reflex_grouped_swiglu
+ *  ws  scratch of >= reflex_swiglu_int8_workspace_size(pair_capacity, E, f)
+ * Errors: NULL pointers; d % 128 or f % 128 nonzero; workspace too small.
+ */
+size_t reflex_swiglu_int8_workspace_size(int pair_capacity, int E, int f);
+int reflex_grouped_swiglu_int8(const int8_t* h, const float* h_scale, const int32_t* sorted_token,
+                               const int32_t* expert_offsets, const int8_t* w_gate,
+                               const int8_t* w_up, const int8_t* w_down, const float* s_gate,
+                               const float* s_up, const float* s_down, int T, int E, int d, int f,
+                               int32_t pair_capacity, uint16_t* y_sorted, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* ---- between blocks --------------------------------------------------------------------
+ * From a block's output and the residual stream to the next block's input.  For each row i:
+ *   y_i = y[i], or from the experts' rows, sum over the pairs j of token i, in rank order, of
+ *         pair_weight[j] y_sorted[pair_to_sorted[j]], plus shared_y[i] when given, in fp32;
+ *         nothing where neither is given
+ *   u_i = residual_scale x_i + gate_i (y_i r(y_i) w_post), rounded to stream_type: x_out[i]
+ *   n_i = u_i r(u_i) w_pre, rounded to bf16: n_out[i]
+ *   q_out[i], q_scale[i]: the row n_i in 8 bits, as reflex_quantize_int8 of n_out gives it
+ * with r(v) = 1 / sqrt(mean of v^2 + eps).  x NULL: no first term; w_post NULL: y_i as it is;
+ * gate NULL: 1; w_pre NULL: no n (then n_out and q_out are NULL).  Products from the left, each
+ * operation rounded to fp32 (the experts' rows by fused multiply-adds); mean and root are taken in
+ * fp64 and r rounded to fp32, so results do not depend on how a row is split.
+ *  x, x_out [T, d] of stream_type (REFLEX_TYPE_*);  y, shared_y, n_out [T, d] bf16;  w_post, w_pre
+ *  [d] fp32;  y_sorted [pair_capacity, d] bf16 with pair_offsets [T+1], pair_to_sorted and
+ *  pair_weight [pair_capacity] as in reflex_combine;  q_out [T, d], q_scale [T]
+ *  gate      [gate_rows, d] bf16: one row (gate_rows 1), one a token (gate_rows T) or, with
+ *            seq_offsets [gate_rows + 1], one for each sequence (rows past the last sequence have
+ *            the last one's)
+ *  n_rows    [1] int32 on the device or NULL: rows from n_rows[0] on are left as they were
+ * x_out may be x; otherwise no output may share memory with an input or another output.
+ * Errors: NULL args or a struct without x, y and y_sorted, without any output, or with some arrays
+ *  of a group alone (pair arrays with y_sorted, q_scale with q_out; n_out or q_out without w_pre)
+ *  (REFLEX_ERR_NULL); y together with y_sorted, w_post, gate or shared_y without an output of the
+ *  block to apply to, unknown stream_type, eps not positive and finite, residual_scale not finite
+ *  (REFLEX_ERR_PARAM); sizes and alignment (REFLEX_ERR_SHAPE; all matrices and weights 16 bytes).
+ */
+typedef struct {
+  int32_t T, d;
+  int32_t stream_type;            /* REFLEX_TYPE_* of x and x_out                         */
+  int32_t gate_rows;
+  int32_t pair_capacity;
+  float   eps;
+  float   residual_scale;
+  int32_t reserved;               /* 0                                                    */
+  const void *x;
+  const uint16_t *y;
+  const uint16_t *y_sorted;
+  const int32_t *pair_offsets, *pair_to_sorted;
+  const float *pair_weight;
+  const uint16_t *shared_y;
+  const float *w_post, *w_pre;
+  const uint16_t *gate;
+  const int32_t *seq_offsets;
+  const int32_t *n_rows;
+  void *x_out;
+  uint16_t *n_out;
+  int8_t *q_out;
+  float *q_scale;
+} reflex_norm_args;
+size_t reflex_sizeof_norm_args(void);         /* sizeof(reflex_norm_args)                       */
+int reflex_block_norm(const reflex_norm_args* args, void* stream);
+
+/*
+ * reflex_moe_forward with the routed and the shared experts in 8-bit integers: the router, the
+ * counts and TopK as there (from the bf16 h), the experts as reflex_grouped_swiglu_int8 on h_q and
+ * h_scale, the 8-bit rows of h that a norm before left (both NULL: h quantised by the call).  The
+ * expert weights of `args` (w_gate .. ws_down) are not read and may be NULL.
+ *  join  NULL: the combine of reflex_moe_forward, to args->out.  Otherwise the experts' rows go on
+ *        through reflex_block_norm(join), which gets them, the pairs and the shared expert's rows
+ *        from the call (its y, y_sorted, pair arrays and shared_y must be NULL; T and d those of
+ *        args; its outputs may be h, h_q and h_scale); args->out, residual_a and residual_b must be
+ *        NULL then.
+ *  ws: >= reflex_workspace_int8_size(T, E, d, f, f_shared, kcap) bytes, 256-byte aligned
+ * Errors: as reflex_moe_forward and, for join, reflex_block_norm; f or f_shared not a multiple of
+ *  128 (REFLEX_ERR_SHAPE); h_q without h_scale or the reverse (REFLEX_ERR_NULL); what must be NULL
+ *  is not, or T or d of join differ (REFLEX_ERR_PARAM).
+ */
+typedef struct {
+  const int8_t *w_gate, *w_up, *w_down;       /* codes [E, f, d], [E, f, d], [E, d, f]          */
+  const float  *s_gate, *s_up, *s_down;       /* their scales [E, f], [E, f], [E, d]            */
+  const int8_t *ws_gate, *ws_up, *ws_down;    /* shared [fs, d], [fs, d], [d, fs] (f_shared > 0) */
+  const float  *ss_gate, *ss_up, *ss_down;
+} reflex_int8_experts;
+size_t reflex_sizeof_int8_experts(void);      /* sizeof(reflex_int8_experts)                    */
+size_t reflex_workspace_int8_size(int T, int E, int d, int f, int f_shared, int k_max);
+int reflex_moe_forward_int8(const reflex_moe_args* args, const reflex_int8_experts* experts,
+                            const int8_t* h_q, const float* h_scale, const reflex_norm_args* join,
+                            void* ws, size_t ws_bytes, void* stream);
+
 /* ---- tokens and confidences ----------------------------------------------------------
  * The token a forward predicts at each position and its confidence c^t (Section 3.1), as
  * reflex_advance_state takes it, from rows of logits and given uniform numbers.

@@ -49,6 +49,20 @@ class Fp8ExpertsC(ctypes.Structure):
                                         "ss_down")]
 
 
+class NormArgsC(ctypes.Structure):
+    """reflex_norm_args: sizes, then the arrays (None: not there)."""
+    _fields_ = ([(n, c_int32) for n in ("T", "d", "stream_type", "gate_rows", "pair_capacity")]
+                + [("eps", c_float), ("residual_scale", c_float), ("reserved", c_int32)]
+                + [(n, c_void_p) for n in ("x", "y", "y_sorted", "pair_offsets", "pair_to_sorted",
+                                           "pair_weight", "shared_y", "w_post", "w_pre", "gate",
+                                           "seq_offsets", "n_rows", "x_out", "n_out", "q_out",
+                                           "q_scale")])
+
+
+class Int8ExpertsC(ctypes.Structure):
+    _fields_ = Fp8ExpertsC._fields_
+
+
 class SampleParamsC(ctypes.Structure):
     """temperature, top_k (0: all), top_p (1: all), min_p (0: all)."""
     _fields_ = [("temperature", c_float), ("top_k", c_int32), ("top_p", c_float),
@@ -98,6 +112,19 @@ _SIGS = {
     "reflex_workspace_fp8_size": (c_size_t, [c_int] * 6),
     "reflex_moe_forward_fp8": (c_int, [ctypes.POINTER(MoeArgsC), ctypes.POINTER(Fp8ExpertsC),
                                        c_void_p, c_size_t, c_void_p]),
+    "reflex_quantize_int8": (c_int, [c_void_p] * 3 + [c_int] * 3 + [c_void_p] * 3),
+    "reflex_quantize_int8_weight": (c_int, [c_void_p] + [c_int] * 3 + [c_void_p] * 3),
+    "reflex_matmul_int8": (c_int, [c_void_p] * 5 + [c_int] * 4 + [c_void_p] * 2),
+    "reflex_swiglu_int8_workspace_size": (c_size_t, [c_int, c_int, c_int]),
+    "reflex_grouped_swiglu_int8": (c_int, [c_void_p] * 10 + [c_int] * 4
+                                   + [c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "reflex_sizeof_norm_args": (c_size_t, []),
+    "reflex_block_norm": (c_int, [ctypes.POINTER(NormArgsC), c_void_p]),
+    "reflex_sizeof_int8_experts": (c_size_t, []),
+    "reflex_workspace_int8_size": (c_size_t, [c_int] * 6),
+    "reflex_moe_forward_int8": (c_int, [ctypes.POINTER(MoeArgsC), ctypes.POINTER(Int8ExpertsC),
+                                        c_void_p, c_void_p, ctypes.POINTER(NormArgsC), c_void_p,
+                                        c_size_t, c_void_p]),
     "reflex_sizeof_sample_params": (c_size_t, []),
     "reflex_sample_workspace_size": (c_size_t, [c_int, c_int]),
     "reflex_sample_tokens": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p,
@@ -127,6 +154,8 @@ def lib():
         if L.reflex_sizeof_moe_args() != ctypes.sizeof(MoeArgsC) or \
                 L.reflex_sizeof_alloc_params() != ctypes.sizeof(AllocParamsC) or \
                 L.reflex_sizeof_fp8_experts() != ctypes.sizeof(Fp8ExpertsC) or \
+                L.reflex_sizeof_int8_experts() != ctypes.sizeof(Int8ExpertsC) or \
+                L.reflex_sizeof_norm_args() != ctypes.sizeof(NormArgsC) or \
                 L.reflex_sizeof_sample_params() != ctypes.sizeof(SampleParamsC):
             raise RuntimeError("libreflex ABI struct layout does not match the binding")
         _lib = L
@@ -478,6 +507,160 @@ def reflex_moe_forward_fp8(args: MoeArgsC, experts: Fp8ExpertsC, ws, stream=None
     """The structs hold addresses: whoever fills them checks the tensors behind (``layer.MoELayer8`` does)."""
     where = "reflex_moe_forward_fp8"
     _launch(where, (ws,), (ctypes.byref(args), ctypes.byref(experts), *space(where, ws)), stream)
+
+
+# --------------------------------------------------------------------------------------
+# 8-bit integer products, norms around a block (checks as above)
+# --------------------------------------------------------------------------------------
+def reflex_quantize_int8(x, q, scale, rows=None, n_rows=None, stream=None):
+    import torch
+    where = "reflex_quantize_int8"
+    M, K = q.shape
+    want(where, "x", x, torch.bfloat16, (None, K))
+    want(where, "q", q, torch.int8, (M, K))
+    want(where, "scale", scale, torch.float32, (M,))
+    if rows is not None:
+        want(where, "rows", rows, torch.int32, (None,))
+        if rows.shape[0] < M:
+            raise ValueError(f"{where}: {rows.shape[0]} rows listed for {M} rows of q")
+    if n_rows is not None:
+        want(where, "n_rows", n_rows, torch.int32, (1,))
+    _launch(where, (x, q, scale, rows, n_rows),
+            (address(x), address(rows), address(n_rows), x.shape[0], M, K, address(q), address(scale)), stream)
+
+
+def reflex_quantize_int8_weight(w, q, scale, stream=None):
+    """w, q [N, K] or [E, N, K]; scale [N] or [E, N]."""
+    import torch
+    where = "reflex_quantize_int8_weight"
+    shape = tuple(w.shape)
+    if len(shape) not in (2, 3):
+        raise ValueError(f"{where}: w has shape {shape}")
+    want(where, "w", w, torch.bfloat16, shape)
+    want(where, "q", q, torch.int8, shape)
+    want(where, "scale", scale, torch.float32, shape[:-1])
+    E, N, K = (1,) * (3 - len(shape)) + shape
+    _launch(where, (w, q, scale), (address(w), E, N, K, address(q), address(scale)), stream)
+
+
+def reflex_matmul_int8(x, x_scale, w, w_scale, out, n_rows=None, stream=None):
+    import torch
+    where = "reflex_matmul_int8"
+    M, K = x.shape
+    N = w.shape[0]
+    want(where, "x", x, torch.int8, (M, K))
+    want(where, "x_scale", x_scale, torch.float32, (M,))
+    want(where, "w", w, torch.int8, (N, K))
+    want(where, "w_scale", w_scale, torch.float32, (N,))
+    want(where, "out", out, (torch.float32, torch.bfloat16), (M, N))
+    if n_rows is not None:
+        want(where, "n_rows", n_rows, torch.int32, (1,))
+    _launch(where, (x, x_scale, w, w_scale, out, n_rows),
+            (address(x), address(x_scale), address(w), address(w_scale), address(n_rows), M, N, K,
+             TYPE_F32 if out.dtype == torch.float32 else TYPE_BF16, address(out)), stream)
+
+
+def reflex_swiglu_int8_workspace_size(pair_capacity, E, f) -> int:
+    return lib().reflex_swiglu_int8_workspace_size(pair_capacity, E, f)
+
+
+def reflex_grouped_swiglu_int8(h, h_scale, sorted_token, expert_offsets, w_gate, w_up, w_down,
+                               s_gate, s_up, s_down, y_sorted, ws, stream=None):
+    import torch
+    where = "reflex_grouped_swiglu_int8"
+    T, d = h.shape
+    E, f, _ = w_gate.shape
+    cap = y_sorted.shape[0]
+    want(where, "h", h, torch.int8, (T, d))
+    want(where, "h_scale", h_scale, torch.float32, (T,))
+    want(where, "sorted_token", sorted_token, torch.int32, (cap,))
+    want(where, "expert_offsets", expert_offsets, torch.int32, (E + 1,))
+    for name, w, s, shape in (("gate", w_gate, s_gate, (E, f, d)), ("up", w_up, s_up, (E, f, d)),
+                              ("down", w_down, s_down, (E, d, f))):
+        want(where, "w_" + name, w, torch.int8, shape)
+        want(where, "s_" + name, s, torch.float32, shape[:2])
+    want(where, "y_sorted", y_sorted, torch.bfloat16, (cap, d))
+    _launch(where, (h, h_scale, sorted_token, expert_offsets, w_gate, w_up, w_down, s_gate, s_up,
+                    s_down, y_sorted, ws),
+            (address(h), address(h_scale), address(sorted_token), address(expert_offsets), address(w_gate), address(w_up),
+             address(w_down), address(s_gate), address(s_up), address(s_down), T, E, d, f, cap, address(y_sorted),
+             *space(where, ws)), stream)
+
+
+def norm_args(where, x=None, y=None, y_sorted=None, pair_offsets=None, pair_to_sorted=None,
+              pair_weight=None, shared_y=None, w_post=None, w_pre=None, gate=None, seq_offsets=None,
+              n_rows=None, x_out=None, n_out=None, q_out=None, q_scale=None, *, eps,
+              residual_scale=1.0):
+    """NormArgsC of checked tensors, and those tensors.  The sizes are those of the first of x, x_out,
+    n_out and q_out that is there."""
+    import torch
+    lead = next((t for t in (x, x_out, n_out, q_out) if t is not None), None)
+    if lead is None:
+        raise ValueError(f"{where}: neither a stream nor an output")
+    shape = lead.shape
+    if len(shape) != 2:
+        raise ValueError(f"{where}: rows of shape {tuple(shape)}, not [T, d]")
+    T, d = shape
+    kind = (x if x is not None else x_out)
+    kind = torch.bfloat16 if kind is None else kind.dtype
+    if kind not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"{where}: a stream of {kind}")
+    cap = 0
+    if x is not None:
+        want(where, "x", x, kind, shape)
+    if y is not None:
+        want(where, "y", y, torch.bfloat16, shape)
+    if y_sorted is not None:
+        want(where, "y_sorted", y_sorted, torch.bfloat16, (None, d))
+        cap = y_sorted.shape[0]
+    for name, t, dtype, size in (("pair_offsets", pair_offsets, torch.int32, T + 1),
+                                 ("pair_to_sorted", pair_to_sorted, torch.int32, cap),
+                                 ("pair_weight", pair_weight, torch.float32, cap),
+                                 ("w_post", w_post, torch.float32, d), ("w_pre", w_pre, torch.float32, d),
+                                 ("n_rows", n_rows, torch.int32, 1), ("q_scale", q_scale, torch.float32, T)):
+        if t is not None:
+            want(where, name, t, dtype, (size,))
+    for name, t, dtype in (("shared_y", shared_y, torch.bfloat16), ("x_out", x_out, kind),
+                           ("n_out", n_out, torch.bfloat16), ("q_out", q_out, torch.int8)):
+        if t is not None:
+            want(where, name, t, dtype, shape)
+    gates = 0
+    if gate is not None:
+        want(where, "gate", gate, torch.bfloat16, (None, d))
+        gates = gate.shape[0]
+    if seq_offsets is not None:
+        want(where, "seq_offsets", seq_offsets, torch.int32, (gates + 1,))
+    tensors = (x, y, y_sorted, pair_offsets, pair_to_sorted, pair_weight, shared_y, w_post, w_pre, gate,
+               seq_offsets, n_rows, x_out, n_out, q_out, q_scale)
+    args = NormArgsC(T, d, TYPE_F32 if kind == torch.float32 else TYPE_BF16, gates, cap, eps, residual_scale, 0,
+                     *[address(t) for t in tensors])
+    return args, (lead, *tensors)
+
+
+def reflex_block_norm(*arrays, stream=None, **named):
+    """Arrays and numbers as in ``norm_args``."""
+    where = "reflex_block_norm"
+    args, tensors = norm_args(where, *arrays, **named)
+    _launch(where, tensors, (ctypes.byref(args),), stream)
+
+
+def reflex_workspace_int8_size(T, E, d, f, f_shared, k_max) -> int:
+    return lib().reflex_workspace_int8_size(T, E, d, f, f_shared, k_max)
+
+
+def reflex_moe_forward_int8(args: MoeArgsC, experts: Int8ExpertsC, ws, h_q=None, h_scale=None,
+                            join: NormArgsC = None, stream=None):
+    """The structs hold addresses: whoever fills them checks the tensors behind (``layer.MoELayerInt8``
+    does)."""
+    import torch
+    where = "reflex_moe_forward_int8"
+    if h_q is not None:
+        want(where, "h_q", h_q, torch.int8, (args.T, args.d))
+    if h_scale is not None:
+        want(where, "h_scale", h_scale, torch.float32, (args.T,))
+    _launch(where, (ws, h_q, h_scale),
+            (ctypes.byref(args), ctypes.byref(experts), address(h_q), address(h_scale),
+             None if join is None else ctypes.byref(join), *space(where, ws)), stream)
 
 
 def reflex_sample_workspace_size(M, V) -> int:

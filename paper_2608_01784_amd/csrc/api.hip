@@ -9,7 +9,7 @@
 #include <mutex>
 #include <vector>
 
-#include "fp8.h"
+#include "int8.h"
 
 using namespace rfx;
 
@@ -193,8 +193,9 @@ class SideFork {
 struct Layout {
   size_t logits, k, done, pair_offsets, pair_expert, pair_weight, expert_offsets, sorted_token,
       pair_to_sorted, perm, route_hist, swiglu, y, shared_act, shared_y, total;
-  size_t h8, h8_scale;      // the 8-bit forward's input rows
+  size_t h8, h8_scale;      // the 8-bit forwards' input rows
 };
+enum class Experts { BF16, FP8, INT8 };
 
 // An always-on expert as wide as the routed ones rides in their two GEMM launches (its rows
 // follow the T * kcap pair rows) up to five pairs per expert at capacity: the fork, the join
@@ -212,10 +213,10 @@ bool shared_joins(int T, int E, int f, int fs, int kcap) {
   return fs == f && static_cast<long long>(T) * std::max(kcap, 1) <= 5LL * E;
 }
 
-bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L, bool fp8 = false) {
+bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L, Experts kind = Experts::BF16) {
   if (!valid_T(T) || !valid_E(E) || !valid_d(d) || !valid_f(f)) return false;
   if (fs != 0 && !valid_f(fs)) return false;
-  if (fp8 && (f % F8_BLOCK != 0 || fs % F8_BLOCK != 0)) return false;
+  if (kind != Experts::BF16 && (f % F8_BLOCK != 0 || fs % F8_BLOCK != 0)) return false;
   if (!valid_kmax(kcap, E)) return false;
   const size_t cap = static_cast<size_t>(T) * kcap;
   if (cap > static_cast<size_t>(INT32_MAX)) return false;
@@ -241,7 +242,9 @@ bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L, bool f
   const bool joins = shared_joins(T, E, f, fs, kcap);
   const size_t rows = cap + (joins ? T : 0);
   auto act_bytes = [&](size_t n, int width) {
-    return fp8 ? swiglu8_ws_bytes(static_cast<int>(n), width) : swiglu_ws_bytes(static_cast<int>(n), width);
+    const int r = static_cast<int>(n);
+    return kind == Experts::BF16 ? swiglu_ws_bytes(r, width)
+                                 : (kind == Experts::FP8 ? swiglu8_ws_bytes(r, width) : swiglu_i8_ws_bytes(r, width));
   };
   if (rows > static_cast<size_t>(INT32_MAX)) return false;
   L.swiglu = take(act_bytes(rows, f));
@@ -249,8 +252,9 @@ bool make_layout(int T, int E, int d, int f, int fs, int kcap, Layout& L, bool f
   L.shared_act = fs && !joins ? take(act_bytes(T, fs)) : o;
   L.shared_y = joins ? L.y + sizeof(uint16_t) * cap * d
                      : (fs ? take(sizeof(uint16_t) * static_cast<size_t>(T) * d) : o);
-  L.h8 = fp8 ? take(static_cast<size_t>(T) * d) : o;
-  L.h8_scale = fp8 ? take(reflex_fp8_scale_bytes(T, d)) : o;
+  L.h8 = kind != Experts::BF16 ? take(static_cast<size_t>(T) * d) : o;
+  L.h8_scale = kind == Experts::FP8 ? take(reflex_fp8_scale_bytes(T, d))
+                                    : (kind == Experts::INT8 ? take(sizeof(float) * static_cast<size_t>(T)) : o);
   L.total = o;
   return true;
 }
@@ -450,16 +454,46 @@ int reflex_combine(const uint16_t* y_sorted, const int32_t* pair_offsets,
                         nullptr, T, d, pair_capacity, out, static_cast<hipStream_t>(stream));
 }
 
+// The 8-bit integer operands of reflex_moe_forward_int8.
+struct Int8Operands {
+  const reflex_int8_experts* experts;
+  const int8_t* h_q;
+  const float* h_scale;
+  const reflex_norm_args* join;
+};
+
+static int check_norm(const reflex_norm_args* a, bool rows_given);
+
 static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes, void* stream,
                             void* const* ev, bool may_fork = true,
-                            const reflex_fp8_experts* x8 = nullptr) {
+                            const reflex_fp8_experts* x8 = nullptr,
+                            const Int8Operands* i8 = nullptr) {
   if (a == nullptr || ws == nullptr) return REFLEX_ERR_NULL;
   const int T = a->T, E = a->E, d = a->d, f = a->f, fs = a->f_shared;
   if (!valid_T(T) || !valid_E(E) || !valid_d(d) || !valid_f(f) || fs < 0 || (fs && !valid_f(fs)))
     return REFLEX_ERR_SHAPE;
   if (a->norm_topk != 0 && a->norm_topk != 1) return REFLEX_ERR_PARAM;
-  RFX_TRY(check_ptrs({a->h, a->w_router, a->out, ws}, 16));
-  if (x8 != nullptr) {
+  const reflex_norm_args* join = i8 != nullptr ? i8->join : nullptr;
+  RFX_TRY(check_ptrs({a->h, a->w_router, ws}, 16));
+  if (join == nullptr) {
+    RFX_TRY(check_ptr(a->out, 16));
+  } else {
+    if (a->out != nullptr || a->residual_a != nullptr || a->residual_b != nullptr || join->T != T || join->d != d)
+      return REFLEX_ERR_PARAM;
+    RFX_TRY(check_norm(join, true));
+  }
+  if (i8 != nullptr) {
+    const reflex_int8_experts& x = *i8->experts;
+    RFX_TRY(check_ptrs({x.w_gate, x.w_up, x.w_down}, 16));
+    RFX_TRY(check_ptrs({x.s_gate, x.s_up, x.s_down}, 4));
+    if (fs) {
+      RFX_TRY(check_ptrs({x.ws_gate, x.ws_up, x.ws_down}, 16));
+      RFX_TRY(check_ptrs({x.ss_gate, x.ss_up, x.ss_down}, 4));
+    }
+    if ((i8->h_q == nullptr) != (i8->h_scale == nullptr)) return REFLEX_ERR_NULL;
+    RFX_TRY(check_opt_ptr(i8->h_q, 16));
+    RFX_TRY(check_opt_ptr(i8->h_scale, 4));
+  } else if (x8 != nullptr) {
     RFX_TRY(check_ptrs({x8->w_gate, x8->w_up, x8->w_down}, 16));
     RFX_TRY(check_ptrs({x8->s_gate, x8->s_up, x8->s_down}, 4));
     if (fs) {
@@ -475,7 +509,7 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
                         static_cast<const void*>(a->k_out), static_cast<const void*>(a->pairs_out),
                         static_cast<const void*>(a->logits_out)})
     RFX_TRY(check_opt_ptr(p, 4));
-  if (fs && x8 == nullptr) RFX_TRY(check_ptrs({a->ws_gate, a->ws_up, a->ws_down}, 16));
+  if (fs && x8 == nullptr && i8 == nullptr) RFX_TRY(check_ptrs({a->ws_gate, a->ws_up, a->ws_down}, 16));
   // pair capacity T * kcap: kcap = uniform_k when set (caller counts are then clamped
   // to it), else params.k_max
   int kcap;
@@ -496,7 +530,8 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
     if (a->B < 0 || a->B > REFLEX_MAX_TOKENS || (T > 0 && a->B < 1)) return REFLEX_ERR_SHAPE;
   }
   Layout L;
-  if (!make_layout(T, E, d, f, fs, kcap, L, x8 != nullptr)) return REFLEX_ERR_SHAPE;
+  const Experts kind = i8 != nullptr ? Experts::INT8 : (x8 != nullptr ? Experts::FP8 : Experts::BF16);
+  if (!make_layout(T, E, d, f, fs, kcap, L, kind)) return REFLEX_ERR_SHAPE;
   if (ws_bytes < L.total) return REFLEX_ERR_WORKSPACE;
   if (T == 0) return REFLEX_OK;
 
@@ -542,7 +577,27 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
     sh8 = Fp8Weights{x8->ws_gate, x8->ws_up, x8->ws_down, x8->ss_gate, x8->ss_up, x8->ss_down};
     RFX_TRY(launch_quantize_rows(a->h, nullptr, nullptr, T, T, d, h8, h8_scale, s));
   }
+  Int8Weights wi{}, shi{};
+  const int8_t* hi = nullptr;
+  const float* hi_scale = nullptr;
+  if (i8 != nullptr) {
+    const reflex_int8_experts& x = *i8->experts;
+    wi = Int8Weights{x.w_gate, x.w_up, x.w_down, x.s_gate, x.s_up, x.s_down};
+    shi = Int8Weights{x.ws_gate, x.ws_up, x.ws_down, x.ss_gate, x.ss_up, x.ss_down};
+    hi = i8->h_q;
+    hi_scale = i8->h_scale;
+    if (hi == nullptr) {
+      int8_t* const q = reinterpret_cast<int8_t*>(h8);
+      float* const qs = reinterpret_cast<float*>(h8_scale);
+      RFX_TRY(launch_quantize_i8(a->h, nullptr, nullptr, T, T, T, d, q, qs, s));
+      hi = q;
+      hi_scale = qs;
+    }
+  }
   auto shared_expert = [&](hipStream_t on) {
+    if (i8 != nullptr)
+      return launch_swiglu_i8(hi, hi_scale, nullptr, nullptr, Int8Weights{}, T, 0, d, fs, 0, AlwaysOnI8{shi, 0, T},
+                              shared_act, shared_y_buf, on);
     if (x8 != nullptr)
       return launch_swiglu8_dense(h8, h8_scale, sh8, T, d, fs, shared_y_buf, reinterpret_cast<uint8_t*>(shared_act), on);
     return launch_swiglu_dense(a->h, a->ws_gate, a->ws_up, a->ws_down, T, d, fs, shared_y_buf, shared_act, on);
@@ -609,7 +664,10 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
                            sorted_token, pair_to_sorted, at(L.perm), s));
   RFX_TRY(mark(4));
   const int sh_rows = joins ? T : 0;
-  if (x8 != nullptr) {
+  if (i8 != nullptr) {
+    RFX_TRY(launch_swiglu_i8(hi, hi_scale, sorted_token, expert_offsets, wi, T, E, d, f, cap, AlwaysOnI8{shi, cap, sh_rows},
+                             act, y, s));
+  } else if (x8 != nullptr) {
     uint8_t* act8 = reinterpret_cast<uint8_t*>(act);
     const AlwaysOn8 on8{sh8, cap, sh_rows};
     RFX_TRY(launch_swiglu8_up(h8, h8_scale, sorted_token, expert_offsets, w8, T, E, d, f, cap, on8, act8, s));
@@ -633,6 +691,16 @@ static int moe_forward_impl(const reflex_moe_args* a, void* ws, size_t ws_bytes,
     shared_y = shared_y_buf;
   }
   RFX_TRY(mark(7));
+  if (join != nullptr) {
+    reflex_norm_args n = *join;
+    n.y_sorted = y;
+    n.pair_offsets = pair_offsets;
+    n.pair_to_sorted = pair_to_sorted;
+    n.pair_weight = pair_weight;
+    n.pair_capacity = cap;
+    n.shared_y = shared_y;
+    return launch_block_norm(n, s);
+  }
   RFX_TRY(launch_combine(y, pair_offsets, pair_to_sorted, pair_weight, shared_y, a->residual_a,
                          a->residual_b, T, d, cap, a->out, s));
   return mark(8);
@@ -768,11 +836,128 @@ int reflex_grouped_swiglu_fp8(const uint8_t* h, const uint8_t* h_scale, const in
   return launch_swiglu8_down(expert_offsets, w, T, E, d, f, pair_capacity, none, act, y_sorted, s);
 }
 
+// ---- 8-bit integers, norms around a block -----------------------------------------------
+int reflex_quantize_int8(const uint16_t* x, const int32_t* rows, const int32_t* n_rows, int x_rows,
+                         int M, int K, int8_t* q, float* scale, void* stream) {
+  RFX_TRY(check_ptrs({x, q}, 16));
+  RFX_TRY(check_ptr(scale, 4));
+  RFX_TRY(check_opt_ptr(rows, 4));
+  RFX_TRY(check_opt_ptr(n_rows, 4));
+  if (!valid_T(x_rows) || !valid_T(M) || !valid_d(K) || (rows == nullptr && x_rows < M))
+    return REFLEX_ERR_SHAPE;
+  if (M == 0) return REFLEX_OK;
+  return launch_quantize_i8(x, rows, n_rows, x_rows, M, M, K, q, scale, static_cast<hipStream_t>(stream));
+}
+
+int reflex_quantize_int8_weight(const uint16_t* w, int E, int N, int K, int8_t* q, float* scale,
+                                void* stream) {
+  RFX_TRY(check_ptrs({w, q}, 16));
+  RFX_TRY(check_ptr(scale, 4));
+  if (!valid_E(E) || !valid_T(N) || !valid_d(K)) return REFLEX_ERR_SHAPE;
+  const size_t rows = static_cast<size_t>(E) * N;
+  if (rows > static_cast<size_t>(INT32_MAX)) return REFLEX_ERR_SHAPE;
+  if (N == 0) return REFLEX_OK;
+  return launch_quantize_i8(w, nullptr, nullptr, rows, rows, rows, K, q, scale, static_cast<hipStream_t>(stream));
+}
+
+int reflex_matmul_int8(const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale,
+                       const int32_t* n_rows, int M, int N, int K, int out_type, void* out,
+                       void* stream) {
+  RFX_TRY(check_ptrs({x, w, out}, 16));
+  RFX_TRY(check_ptrs({x_scale, w_scale}, 4));
+  RFX_TRY(check_opt_ptr(n_rows, 4));
+  if (!valid_T(M) || !valid_T(N) || !valid_d(K)) return REFLEX_ERR_SHAPE;
+  if (out_type != REFLEX_TYPE_BF16 && out_type != REFLEX_TYPE_F32) return REFLEX_ERR_PARAM;
+  if (M == 0 || N == 0) return REFLEX_OK;
+  return launch_matmul_i8(x, x_scale, w, w_scale, n_rows, M, N, K, out_type, out, static_cast<hipStream_t>(stream));
+}
+
+size_t reflex_swiglu_int8_workspace_size(int pair_capacity, int E, int f) {
+  if (pair_capacity < 0 || !valid_E(E) || !valid_f(f) || f % F8_BLOCK != 0) return 0;
+  return swiglu_i8_ws_bytes(pair_capacity, f);
+}
+
+int reflex_grouped_swiglu_int8(const int8_t* h, const float* h_scale, const int32_t* sorted_token,
+                               const int32_t* expert_offsets, const int8_t* w_gate,
+                               const int8_t* w_up, const int8_t* w_down, const float* s_gate,
+                               const float* s_up, const float* s_down, int T, int E, int d, int f,
+                               int32_t pair_capacity, uint16_t* y_sorted, void* ws,
+                               size_t ws_bytes, void* stream) {
+  RFX_TRY(check_ptrs({h, w_gate, w_up, w_down, y_sorted, ws}, 16));
+  RFX_TRY(check_ptrs({h_scale, s_gate, s_up, s_down, sorted_token, expert_offsets}, 4));
+  if (!valid_T(T) || !valid_E(E) || !valid_d(d) || !valid_f(f) || f % F8_BLOCK != 0 || pair_capacity < 0)
+    return REFLEX_ERR_SHAPE;
+  if (ws_bytes < swiglu_i8_ws_bytes(pair_capacity, f)) return REFLEX_ERR_WORKSPACE;
+  if (T == 0 || pair_capacity == 0) return REFLEX_OK;
+  return launch_swiglu_i8(h, h_scale, sorted_token, expert_offsets, Int8Weights{w_gate, w_up, w_down, s_gate, s_up, s_down},
+                          T, E, d, f, pair_capacity, AlwaysOnI8{}, ws, y_sorted, static_cast<hipStream_t>(stream));
+}
+
+size_t reflex_sizeof_norm_args(void) { return sizeof(reflex_norm_args); }
+
+// rows_given: the experts' rows come from the caller (reflex_moe_forward_int8's own).
+static int check_norm(const reflex_norm_args* a, bool rows_given) {
+  if (a == nullptr) return REFLEX_ERR_NULL;
+  const bool wide = a->stream_type == REFLEX_TYPE_F32, pairs = a->y_sorted != nullptr;
+  if (!wide && a->stream_type != REFLEX_TYPE_BF16) return REFLEX_ERR_PARAM;
+  if (!(a->eps > 0.0f) || !std::isfinite(a->eps) || !std::isfinite(a->residual_scale)) return REFLEX_ERR_PARAM;
+  const bool any_pair = pairs || a->pair_offsets != nullptr || a->pair_to_sorted != nullptr || a->pair_weight != nullptr;
+  const bool block = a->y != nullptr || pairs || rows_given;
+  if (rows_given && (a->y != nullptr || any_pair || a->shared_y != nullptr)) return REFLEX_ERR_PARAM;
+  if (any_pair && (!pairs || a->pair_offsets == nullptr || a->pair_to_sorted == nullptr || a->pair_weight == nullptr))
+    return REFLEX_ERR_NULL;
+  if (pairs && a->y != nullptr) return REFLEX_ERR_PARAM;
+  if (a->shared_y != nullptr && !pairs) return REFLEX_ERR_PARAM;
+  if (!block && a->x == nullptr) return REFLEX_ERR_NULL;
+  if (!block && (a->w_post != nullptr || a->gate != nullptr)) return REFLEX_ERR_PARAM;
+  if (a->x_out == nullptr && a->n_out == nullptr && a->q_out == nullptr) return REFLEX_ERR_NULL;
+  if ((a->q_out == nullptr) != (a->q_scale == nullptr)) return REFLEX_ERR_NULL;
+  if (a->w_pre == nullptr && (a->n_out != nullptr || a->q_out != nullptr)) return REFLEX_ERR_NULL;
+  if (a->seq_offsets != nullptr && a->gate == nullptr) return REFLEX_ERR_NULL;
+  for (const void* p : {a->x, static_cast<const void*>(a->y), static_cast<const void*>(a->y_sorted),
+                        static_cast<const void*>(a->shared_y), static_cast<const void*>(a->w_post),
+                        static_cast<const void*>(a->w_pre), static_cast<const void*>(a->gate),
+                        static_cast<const void*>(a->x_out), static_cast<const void*>(a->n_out),
+                        static_cast<const void*>(a->q_out)})
+    RFX_TRY(check_opt_ptr(p, 16));
+  for (const void* p : {static_cast<const void*>(a->pair_offsets), static_cast<const void*>(a->pair_to_sorted),
+                        static_cast<const void*>(a->pair_weight), static_cast<const void*>(a->seq_offsets),
+                        static_cast<const void*>(a->n_rows), static_cast<const void*>(a->q_scale)})
+    RFX_TRY(check_opt_ptr(p, 4));
+  if (!valid_T(a->T) || !valid_d(a->d) || (pairs && a->pair_capacity < 0)) return REFLEX_ERR_SHAPE;
+  if (a->gate != nullptr && a->T > 0) {
+    if (a->gate_rows < 1 || a->gate_rows > REFLEX_MAX_TOKENS) return REFLEX_ERR_SHAPE;
+    if (a->seq_offsets == nullptr && a->gate_rows != 1 && a->gate_rows != a->T) return REFLEX_ERR_SHAPE;
+  }
+  return REFLEX_OK;
+}
+
+int reflex_block_norm(const reflex_norm_args* args, void* stream) {
+  RFX_TRY(check_norm(args, false));
+  if (args->T == 0) return REFLEX_OK;
+  return launch_block_norm(*args, static_cast<hipStream_t>(stream));
+}
+
+size_t reflex_sizeof_int8_experts(void) { return sizeof(reflex_int8_experts); }
+
+size_t reflex_workspace_int8_size(int T, int E, int d, int f, int f_shared, int k_max) {
+  Layout L;
+  return make_layout(T, E, d, f, f_shared, k_max, L, Experts::INT8) ? L.total : 0;
+}
+
+int reflex_moe_forward_int8(const reflex_moe_args* args, const reflex_int8_experts* experts,
+                            const int8_t* h_q, const float* h_scale, const reflex_norm_args* join,
+                            void* ws, size_t ws_bytes, void* stream) {
+  if (experts == nullptr) return REFLEX_ERR_NULL;
+  const Int8Operands operands{experts, h_q, h_scale, join};
+  return moe_forward_impl(args, ws, ws_bytes, stream, nullptr, true, nullptr, &operands);
+}
+
 size_t reflex_sizeof_fp8_experts(void) { return sizeof(reflex_fp8_experts); }
 
 size_t reflex_workspace_fp8_size(int T, int E, int d, int f, int f_shared, int k_max) {
   Layout L;
-  return make_layout(T, E, d, f, f_shared, k_max, L, true) ? L.total : 0;
+  return make_layout(T, E, d, f, f_shared, k_max, L, Experts::FP8) ? L.total : 0;
 }
 
 int reflex_moe_forward_fp8(const reflex_moe_args* args, const reflex_fp8_experts* experts, void* ws,
