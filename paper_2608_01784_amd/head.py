@@ -1,8 +1,9 @@
 """The end of a denoising forward: tokens and confidences of the masked positions.
 
 Only the positions that are still masked need logits.  ``TokenHead`` lists them on the GPU
-(``reflex_select_rows``), rounds their hidden states to 8 bits (``reflex_quantize_fp8``),
-multiplies them with the 8-bit head weights (``reflex_matmul_fp8``) and draws a token and its
+(``reflex_select_rows``), rounds their hidden states to 8 bits (``reflex_quantize_fp8``, with
+integer weights ``reflex_quantize_int8``), multiplies them with the 8-bit head weights
+(``reflex_matmul_fp8``, ``reflex_matmul_int8``) and draws a token and its
 confidence from each row of logits (``reflex_sample_tokens``).  The host never learns how many
 rows there are: nothing is copied back and the launches can be captured.
 """
@@ -20,7 +21,7 @@ class TokenHead:
     """Buffers and 8-bit weights of a head for T positions.
 
     weight: bf16 [V, d], rounded to 8 bits here, or a pair of codes and scales as
-    ``quantize_weight`` gives them.  tokens int32 [T] and conf float32 [T] hold the last
+    ``quantize_weight`` or ``quantize_weight_int8`` gives them.  tokens int32 [T] and conf float32 [T] hold the last
     prediction at every position: -1 and 0 until there is one, and from the forward that
     commits a position on what that forward predicted.  logits: [T, V], the masked positions'
     rows in front (room for all of them: 4.3 GB for 8192 positions of 131072 tokens in fp32)."""
@@ -34,8 +35,13 @@ class TokenHead:
         dev = self.w.device
         self.rows = torch.empty(T, dtype=torch.int32, device=dev)
         self.n_rows = torch.zeros(1, dtype=torch.int32, device=dev)
-        self.q = torch.empty((T, d), dtype=torch.float8_e4m3fn, device=dev)
-        self.scale = torch.empty(_lib.fp8_scale_shape(T, d), dtype=torch.uint8, device=dev)
+        self.integers = self.w.dtype == torch.int8
+        if self.integers:
+            self.q = torch.empty((T, d), dtype=torch.int8, device=dev)
+            self.scale = torch.empty(T, dtype=torch.float32, device=dev)
+        else:
+            self.q = torch.empty((T, d), dtype=torch.float8_e4m3fn, device=dev)
+            self.scale = torch.empty(_lib.fp8_scale_shape(T, d), dtype=torch.uint8, device=dev)
         self.logits = torch.empty((T, V), dtype=logits_dtype, device=dev)
         self.tokens = torch.full((T,), -1, dtype=torch.int32, device=dev)
         self.conf = torch.zeros(T, dtype=torch.float32, device=dev)
@@ -49,8 +55,10 @@ class TokenHead:
             raise ValueError(f"TokenHead: x {tuple(x.shape)} and masked {tuple(masked.shape)} "
                              f"for {self.T} positions of {self.d}")
         _lib.reflex_select_rows(masked, self.rows, self.n_rows, ws=self.ws, stream=stream)
-        _lib.reflex_quantize_fp8(x, self.q, self.scale, self.rows, self.n_rows, stream=stream)
-        _lib.reflex_matmul_fp8(self.q, self.scale, self.w, self.w_scale, self.logits, self.n_rows, stream=stream)
+        quantize = _lib.reflex_quantize_int8 if self.integers else _lib.reflex_quantize_fp8
+        multiply = _lib.reflex_matmul_int8 if self.integers else _lib.reflex_matmul_fp8
+        quantize(x, self.q, self.scale, self.rows, self.n_rows, stream=stream)
+        multiply(self.q, self.scale, self.w, self.w_scale, self.logits, self.n_rows, stream=stream)
         _lib.reflex_sample_tokens(self.logits, u, self.params, self.tokens, self.conf, self.rows, self.n_rows,
                                   ws=self.ws, stream=stream)
         return self.tokens, self.conf

@@ -126,6 +126,14 @@ def quantize_weight(w: torch.Tensor, stream=None):
     return q, scale
 
 
+def quantize_weight_int8(w: torch.Tensor, stream=None):
+    """Integer codes and scales of bf16 weights [N, K] or [E, N, K] (``reflex_quantize_int8_weight``)."""
+    q = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+    scale = torch.empty(w.shape[:-1], dtype=torch.float32, device=w.device)
+    _lib.reflex_quantize_int8_weight(w, q, scale, stream=stream)
+    return q, scale
+
+
 @dataclass
 class ExpertWeights8:
     """8-bit expert weights, shapes as in ExpertWeights: codes (float8_e4m3fn or uint8) and their
@@ -149,20 +157,26 @@ class ExpertWeights8:
     f = ExpertWeights.f
     f_shared = ExpertWeights.f_shared
 
+    # what the codes and their scales are
+    _codes = staticmethod(_lib.code_types)
+    _scales = torch.uint8
+    _scale_shape = staticmethod(_lib.fp8_weight_scale_shape)
+    _rounded = staticmethod(quantize_weight)
+
     @classmethod
     def quantize(cls, w: ExpertWeights, stream=None) -> "ExpertWeights8":
         """The bf16 weights rounded to 8 bits (the router is shared, not copied)."""
         made = {"w_router": w.w_router, "router_bias": w.router_bias}
         for name in ("gate", "up", "down"):
-            made["w_" + name], made["s_" + name] = quantize_weight(getattr(w, "w_" + name), stream)
+            made["w_" + name], made["s_" + name] = cls._rounded(getattr(w, "w_" + name), stream)
             shared = getattr(w, "ws_" + name)
             if shared is not None:
-                made["ws_" + name], made["ss_" + name] = quantize_weight(shared, stream)
+                made["ws_" + name], made["ss_" + name] = cls._rounded(shared, stream)
         return cls(**made)
 
     def check(self, d: int):
         """Shapes, types, density and device of all weights (the C call sees addresses alone)."""
-        where, E, f, fs = "ExpertWeights8", self.E, self.f, self.f_shared
+        where, E, f, fs = type(self).__name__, self.E, self.f, self.f_shared
         sets = [("w_", "s_", (E, f, d), (E, d, f))]
         if fs:
             sets.append(("ws_", "ss_", (fs, d), (d, fs)))
@@ -171,8 +185,8 @@ class ExpertWeights8:
                 w, s = getattr(self, codes + name), getattr(self, scales + name)
                 if w is None or s is None:
                     raise ValueError(f"{where}: {codes + name} without all of its tensors")
-                _lib.want(where, codes + name, w, _lib.code_types(), shape)
-                _lib.want(where, scales + name, s, torch.uint8, _lib.fp8_weight_scale_shape(*shape))
+                _lib.want(where, codes + name, w, self._codes(), shape)
+                _lib.want(where, scales + name, s, self._scales, self._scale_shape(*shape))
                 if w.device != self.w_router.device or s.device != self.w_router.device:
                     raise ValueError(f"{where}: {codes + name} on {w.device}, the router on {self.w_router.device}")
         _lib.want(where, "w_router", self.w_router, torch.float32, (E, d))
@@ -189,6 +203,16 @@ class ExpertWeights8:
         return all_, tuple(_lib.ptr(t) for t in all_)
 
 
+@dataclass
+class ExpertWeightsInt8(ExpertWeights8):
+    """Expert weights as 8-bit integers, shapes as in ExpertWeights: codes (int8) and a float32 scale for each
+    output channel (their shapes without the last dimension); the router stays fp32."""
+    _codes = staticmethod(lambda: (torch.int8,))
+    _scales = torch.float32
+    _scale_shape = staticmethod(lambda *shape: shape[:-1])
+    _rounded = staticmethod(quantize_weight_int8)
+
+
 class MoELayer8(MoELayer):
     """MoELayer with the experts in 8 bits (``reflex_moe_forward_fp8``): hidden states come in and go
     out in bf16, router, counts, TopK and combine are the same.
@@ -202,7 +226,7 @@ class MoELayer8(MoELayer):
         weights.check(d)
         at = weights.w_router.device
         if device is not None and torch.empty(0, device=device).device != at:
-            raise ValueError(f"MoELayer8: device {device}, but weights on {at}")
+            raise ValueError(f"{type(self).__name__}: device {device}, but weights on {at}")
         super().__init__(T, d, weights, params, uniform_k, norm_topk, k_rule, k_threshold, at)
         self._sizes = (weights.E, weights.f, weights.f_shared)
         self._set_experts(*weights.tensors())
@@ -216,7 +240,7 @@ class MoELayer8(MoELayer):
         return _lib.reflex_workspace_fp8_size(self.T, w.E, self.d, w.f, w.f_shared, self.kcap)
 
     def _check(self, h, state, k_in, residual_a, residual_b, out):
-        w, where, T = self.w, "MoELayer8", self.T
+        w, where, T = self.w, type(self).__name__, self.T
         tensors, addresses = w.tensors()
         # replaced: other tensors, or the same ones with other memory
         if addresses != self._addresses or any(a is not b for a, b in zip(tensors, self._checked)):
@@ -268,3 +292,80 @@ class MoELayer8(MoELayer):
         else:               # (the call enqueues nothing)
             self.pairs.zero_()
         return self.out if out is None else out
+
+
+class MoELayerInt8(MoELayer8):
+    """MoELayer8 with the experts in 8-bit integers (``reflex_moe_forward_int8``).
+
+    h_q, h_scale: the 8-bit rows of h where a norm before has left them (``BlockNorm``); h is rounded by the call
+    otherwise.  join: arrays and numbers of ``_lib.norm_args`` (as ``BlockNorm.arrays`` gives them) without a
+    block's output: the experts' rows then go on through that norm in place of the combine, and the result is the
+    next block's input, or the stream where the norm leaves no input."""
+
+    def _set_experts(self, tensors, addresses):
+        super()._set_experts(tensors, addresses)
+        self.experts = _lib.Int8ExpertsC(*addresses[:12])
+
+    def _workspace_bytes(self) -> int:
+        w = self.w
+        return _lib.reflex_workspace_int8_size(self.T, w.E, self.d, w.f, w.f_shared, self.kcap)
+
+    def forward(self, h, state=None, k_in=None, residual_a=None, residual_b=None, out=None, stream=None, h_q=None,
+                h_scale=None, join=None) -> torch.Tensor:
+        where = type(self).__name__
+        args = self.args(h, state, k_in, residual_a, residual_b, out)
+        norm, to = None, self.out if out is None else out
+        if join is not None:
+            if out is not None or residual_a is not None or residual_b is not None:
+                raise ValueError(f"{where}: out and residuals belong to the combine, which join takes the place of")
+            norm, tensors = _lib.norm_args(where, **join)
+            if (norm.T, norm.d) != (self.T, self.d):
+                raise ValueError(f"{where}: join of {norm.T} rows of {norm.d}, the layer of {self.T} of {self.d}")
+            if any(t is not None and t.get_device() != self.ws.get_device() for t in tensors):
+                raise ValueError(f"{where}: join with tensors on another device than {self.ws.device}")
+            args.out = None
+            to = join.get("x_out") if join.get("n_out") is None else join["n_out"]
+        if self.T > 0:      # (empty tensors have no address)
+            _lib.reflex_moe_forward_int8(args, self.experts, self.ws, h_q, h_scale, norm, stream)
+        else:               # (the call enqueues nothing)
+            self.pairs.zero_()
+        return to
+
+
+class BlockNorm:
+    """What stands between a block's output and the next block's input (``reflex_block_norm``), with buffers for T
+    rows of d: n bf16 [T, d], and with `quantize` its 8-bit rows q int8 [T, d], scale float32 [T].
+
+    w_post, w_pre: float32 [d], the weights of the norm after the block and before the next (w_pre None: no next
+    input, the stream alone)."""
+
+    def __init__(self, T: int, d: int, w_pre=None, w_post=None, eps: float = 1e-6, residual_scale: float = 1.0,
+                 quantize: bool = True, device=None):
+        at = next((w.device for w in (w_pre, w_post) if w is not None), "cuda" if device is None else device)
+        self.T, self.d, self.w_pre, self.w_post = int(T), int(d), w_pre, w_post
+        self.eps, self.residual_scale = float(eps), float(residual_scale)
+        self.n = self.q = self.scale = None
+        if w_pre is not None:
+            self.n = torch.empty((T, d), dtype=torch.bfloat16, device=at)
+            if quantize:
+                self.q = torch.empty((T, d), dtype=torch.int8, device=at)
+                self.scale = torch.empty(T, dtype=torch.float32, device=at)
+
+    def arrays(self, x, gate=None, seq_offsets=None, n_rows=None, x_out=None) -> dict:
+        """Arguments of ``reflex_block_norm`` without a block's output.  x: the stream, bf16 or float32 [T, d],
+        replaced in place unless there is an x_out (None: no stream yet, x_out takes the first)."""
+        return dict(x=x, w_post=self.w_post, w_pre=self.w_pre, gate=gate, seq_offsets=seq_offsets, n_rows=n_rows,
+                    x_out=x if x_out is None else x_out, n_out=self.n, q_out=self.q, q_scale=self.scale, eps=self.eps,
+                    residual_scale=self.residual_scale)
+
+    def forward(self, x, y, gate=None, seq_offsets=None, n_rows=None, x_out=None, stream=None):
+        """The block's output y (bf16 [T, d]) into the stream; returns the next block's input (None without a
+        norm before)."""
+        _lib.reflex_block_norm(y=y, stream=stream, **self.arrays(x, gate, seq_offsets, n_rows, x_out))
+        return self.n
+
+    def start(self, x, n_rows=None, stream=None):
+        """The norm before the first block: the input from the stream, which stays as it is."""
+        _lib.reflex_block_norm(x=x, w_pre=self.w_pre, n_rows=n_rows, n_out=self.n, q_out=self.q, q_scale=self.scale,
+                               eps=self.eps, stream=stream)
+        return self.n
