@@ -26,9 +26,7 @@ __device__ __forceinline__ void add_bf16x8(float* acc, uint4 v, float w) {
 // Kernel durations traced in one process, identical output: skewed layer (656 MB) 130.3
 // -> 109.3 us; 16-layer stack layer with its two residual streams (276 MB) 51.2 -> 50.1
 // us; with the hint where the streams fit: stack layer without residuals (209 MB) 35.4
-// -> 36.2 us, LLaDA2.0-mini with residuals (152 MB) 28.3 -> 30.3 us.
-constexpr size_t kStreamBytes = size_t(256) << 20;
-
+// -> 36.2 us, LLaDA2.0-mini with residuals (152 MB) 28.3 -> 30.3 us.  (kStreamBytes)
 typedef unsigned int u32x4_nt __attribute__((ext_vector_type(4)));
 
 template <bool STREAM>

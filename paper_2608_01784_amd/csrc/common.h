@@ -12,6 +12,7 @@
 namespace rfx {
 
 constexpr int kWave = 64;
+constexpr size_t kStreamBytes = size_t(256) << 20;      // the Infinity Cache
 
 // ---- bf16 <-> fp32 ------------------------------------------------------------------
 RFX_DEVICE float bf16_to_f32(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
