@@ -38,7 +38,7 @@
 // ahead continues across tile boundaries.  Tiles are dealt to the 8 XCDs in contiguous runs
 // (workgroup b runs on XCD b % 8).  Of an expert the N tiles of one M tile are adjacent (its
 // gathered rows stay in L2); of a plain product the M tiles of one N tile (the weights are the
-// large operand).
+// large operand), of integers within strips of M tiles.
 //
 // What bounds it, measured: many rows by the MFMAs (8192 x 8192 x 8192 2.3 PFLOP/s, where a large
 // library product of this type reaches 2.7) and, with a short K, by the tiles' stores, which come from all
@@ -74,6 +74,11 @@ constexpr int G8_BK = F8_BLOCK;                  // bytes of a slice's row
 constexpr int G8_CHUNKS = G8_BK / 16;
 constexpr int G8_OP_ROWS = 64 / G8_CHUNKS;       // rows of one wave's copy (1 KB)
 constexpr int G8_NJ = 4;                         // 32-row weight blocks per wave
+// M tiles of a strip of a plain product of integers: an XCD's 32 workgroups then have 8 x 4 tiles, whose rows and
+// weights it reads from L2 (all tiles of a strip start with the same K), where 32 M tiles of one N tile pass L2 by.
+// 8192^3 463 -> 440 us, 8192 x 8192 x 2048 136 -> 130, 4096^3 with fp32 results 66.7 -> 65.3 (strips of 4 and 16: 439 and
+// 448, 130 and 133).
+constexpr int G8_STRIP = 8;
 enum Mode { UP, DOWN, PLAIN };
 enum Codes { F8, I8 };
 
@@ -181,7 +186,8 @@ __device__ __forceinline__ uint32_t stage_at(uint32_t stage, int row, int chunk)
 // The staged 32 rows x (128 / sizeof(OUT)) columns to `out`: rows row_base .. below row_end, columns
 // col_base .. below N.  8 lanes a row, 16 bytes each, at any address that the elements allow (rows of
 // an odd N start anywhere; global stores need no alignment beyond that).
-template <class OUT, bool ANY_N>
+// (STREAM: whole vectors that pass the caches by)
+template <class OUT, bool ANY_N, bool STREAM = false>
 __device__ __forceinline__ void store_staged(int row_base, int col_base, int row_end, int N, OUT* __restrict__ out,
                                              uint32_t stage) {
   constexpr int VEC = 16 / sizeof(OUT), COLS = 128 / sizeof(OUT);
@@ -220,7 +226,13 @@ __device__ __forceinline__ void store_staged(int row_base, int col_base, int row
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int row = row_base + (lane >> 3) + 8 * q;
-    if (row < row_end && col < N) __builtin_memcpy(out + static_cast<size_t>(row) * N + col, &v[q], 16);
+    if (row < row_end && col < N) {
+      OUT* const to = out + static_cast<size_t>(row) * N + col;
+      if constexpr (STREAM)
+        __builtin_nontemporal_store(v[q], reinterpret_cast<u32x4_t*>(to));
+      else
+        __builtin_memcpy(to, &v[q], 16);
+    }
   }
 }
 
@@ -320,13 +332,22 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
     Tile t;
     if (MODE == PLAIN || always_on) {
       // (PLAIN: M inner; an always-on expert: N inner, as the routed ones)
-      const int n = MODE == PLAIN ? L / sh_m : L % n_tiles, m = MODE == PLAIN ? L - n * sh_m : L / n_tiles;
+      int n = MODE == PLAIN ? L / sh_m : L % n_tiles, m = MODE == PLAIN ? L - n * sh_m : L / n_tiles;
+      bool strip = false;
+      if constexpr (CODES == I8 && MODE == PLAIN) {
+        strip = sh_m > G8_STRIP;
+        if (strip) {
+          const int g = L / (G8_STRIP * n_tiles), high = min(G8_STRIP, sh_m - g * G8_STRIP), l = L - g * G8_STRIP * n_tiles;
+          n = l / high;
+          m = g * G8_STRIP + l - n * high;
+        }
+      }
       const int height = height_of(sh_rows, sh_m);
       t.expert = E;
       t.n0 = n * BN;
       t.row0 = a.sh_row0 + min(m * height, sh_rows);
       t.row_end = min(a.sh_row0 + sh_rows, t.row0 + height);
-      t.rot = n % groups;
+      t.rot = strip ? 0 : n % groups;
       return t;
     }
     int e = -1;      // four ballots count the experts whose first tile lies at or before L
@@ -353,11 +374,30 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
   const int run_tiles = (MODE == PLAIN ? sh_m : m_total) * n_tiles;
   const int chunk = (run_tiles + G8_XCDS - 1) / G8_XCDS;
   const int r_begin = xcd * chunk, r_mine = max(min(run_tiles - r_begin, chunk), 0);
-  if (j0 >= sh_mine + r_mine) return;
-  const int n_my = (sh_mine + r_mine - j0 + per_xcd - 1) / per_xcd;
+  // Plain products of integers: where the XCD's last round has tiles for a half or a quarter of its workgroups, those are
+  // cut by rows into two or four (1024 x 50257 x 2048, 3.08 rounds, 130 -> 124 us; experts' tiles are uneven as they are:
+  // 53000 rows of 64 experts 474 and 476).
+  const int mine = sh_mine + r_mine, last = mine / per_xcd * per_xcd, rest = mine - last;
+  int parts = 1;
+  if (CODES == I8 && MODE == PLAIN && MI > 1 && last > 0 && rest > 0)
+    parts = MI > 2 && 4 * rest <= per_xcd ? 4 : (2 * rest <= per_xcd ? 2 : 1);
+  const int items = last + rest * parts;
+  if (j0 >= items) return;
+  const int n_my = (items - j0 + per_xcd - 1) / per_xcd;
   auto tile_at = [&](int i) {
-    const int j = j0 + i * per_xcd;
-    return j < sh_mine ? decode(true, xcd + G8_XCDS * j) : decode(false, r_begin + j - sh_mine);
+    int j = j0 + i * per_xcd, part = 0;
+    const bool cut = CODES == I8 && MODE == PLAIN && parts > 1 && j >= last;
+    if (cut) {
+      part = (j - last) % parts;
+      j = last + (j - last) / parts;
+    }
+    Tile t = j < sh_mine ? decode(true, xcd + G8_XCDS * j) : decode(false, r_begin + j - sh_mine);
+    if (cut) {
+      const int height = ((t.row_end - t.row0 + parts - 1) / parts + 63) & ~63;
+      t.row0 = min(t.row0 + part * height, t.row_end);
+      t.row_end = min(t.row0 + height, t.row_end);
+    }
+    return t;
   };
   // ---- copies: op q of a slice fills rows OP_ROWS q ..; lane L writes row r = OP_ROWS q + L / 8 at
   // slot L % 8, holding chunk (L % 8) ^ ((r / 2) % 8).  Each loader (input rows, weights) has a
@@ -779,22 +819,28 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
     const int el = lane_here(), erow = el & 31, esel = el >> 5;
     if constexpr (CODES == I8) {
       // The wave's column scales, through LDS into each lane's 4 x 16 columns; then a pair block at a time: the sums
-      // times both scales (UP: the activation of gate and up), staged and stored as below.
+      // times both scales (UP: the activation of gate and up), staged and stored as below.  Experts' rows pass the caches
+      // by, which leaves those to the weights' stream (experts of 1024 / 8192 tokens, E = 64, 120 -> 112 and 453 -> 448 us;
+      // the whole layer with its norm 157 -> 154 and 569 -> 567, E = 256 249 -> 246).
       if constexpr (NB > 0) {
         const uint32_t mine = scratch + S::WAVES * G8_STAGE + wave * 512;
         asm volatile("ds_write_b32 %0, %1\n\tds_write_b32 %0, %2 offset:256\n\ts_waitcnt lgkmcnt(0)" ::"v"(mine + 4 * el),
                      "v"(w_cur[0]), "v"(w_cur[1])
                      : "memory");
-        f32x4_t sw[G8_NJ][4];      // (UP: block j's columns 32 (j % 2) .. of gate, j < 2, or up)
-#pragma unroll
-        for (int j = 0; j < G8_NJ; ++j) {
+        auto columns = [&](int j, f32x4_t (&w)[4]) {      // the scales of the lane's columns in block j
           const uint32_t at = mine + 128 * j + 16 * esel;
           asm volatile(
               "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\t"
               "ds_read_b128 %3, %4 offset:96\n\ts_waitcnt lgkmcnt(0)"
-              : "=&v"(sw[j][0]), "=&v"(sw[j][1]), "=&v"(sw[j][2]), "=&v"(sw[j][3])
+              : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3])
               : "v"(at)
               : "memory");
+        };
+        // (UP: read again for every pair block, two gate and up blocks at a time, which leaves the activation registers)
+        f32x4_t sw[G8_NJ][4];
+        if constexpr (MODE != UP) {
+#pragma unroll
+          for (int j = 0; j < G8_NJ; ++j) columns(j, sw[j]);
         }
         uint32_t sxb[MI];
         rows_scales(sxb);
@@ -808,14 +854,18 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
           auto value = [&](int j, int r) { return static_cast<float>(acc[i][j][r]) * (sx * sw[j][r / 4][r % 4]); };
           if constexpr (MODE == UP) {
 #pragma unroll
-            for (int jj = 0; jj < 2; ++jj)
+            for (int jj = 0; jj < 2; ++jj) {
+              __builtin_amdgcn_sched_barrier(0);
+              columns(jj, sw[jj]);
+              columns(jj + 2, sw[jj + 2]);
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 auto act = [&](int r) { return silu_mul(value(jj, 4 * g + r), value(jj + 2, 4 * g + r)); };
                 lds_write64(stage_at(stage, erow, 4 * jj + g) + 8 * esel, pack_bf16x2(act(0), act(1)),
                             pack_bf16x2(act(2), act(3)));
               }
-            store_staged<OUT, false>(rb, t.n0 + 64 * wn, t.row_end, N, out, stage);
+            }
+            store_staged<OUT, false, true>(rb, t.n0 + 64 * wn, t.row_end, N, out, stage);
           } else {
 #pragma unroll
             for (int j = 0; j < G8_NJ; j += sizeof(OUT) == 4 ? 1 : 2) {
@@ -834,7 +884,7 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
                                 pack_bf16x2(value(j + jj, 4 * g), value(j + jj, 4 * g + 1)),
                                 pack_bf16x2(value(j + jj, 4 * g + 2), value(j + jj, 4 * g + 3)));
               }
-              store_staged<OUT, MODE == PLAIN>(rb, t.n0 + 128 * wn + 32 * j, t.row_end, N, out, stage);
+              store_staged<OUT, MODE == PLAIN, MODE == DOWN>(rb, t.n0 + 128 * wn + 32 * j, t.row_end, N, out, stage);
             }
           }
         }
