@@ -379,7 +379,7 @@ def _launch(where, tensors, args, stream):
     fn = getattr(lib(), where)
     # (the current stream's handle without a stream object: 0.1 us, not 2.9 of a small call's 10)
     handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():      # (torch is initialised: there is a device tensor)
         _check(fn(*args, handle), where)
     else:
         with torch.cuda.device(index):
@@ -594,47 +594,48 @@ def norm_args(where, x=None, y=None, y_sorted=None, pair_offsets=None, pair_to_s
     """NormArgsC of checked tensors, and those tensors.  The sizes are those of the first of x, x_out,
     n_out and q_out that is there."""
     import torch
-    lead = next((t for t in (x, x_out, n_out, q_out) if t is not None), None)
+    b16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    lead = x if x is not None else x_out if x_out is not None else n_out if n_out is not None else q_out
     if lead is None:
         raise ValueError(f"{where}: neither a stream nor an output")
     shape = lead.shape
     if len(shape) != 2:
         raise ValueError(f"{where}: rows of shape {tuple(shape)}, not [T, d]")
     T, d = shape
-    kind = (x if x is not None else x_out)
-    kind = torch.bfloat16 if kind is None else kind.dtype
-    if kind not in (torch.bfloat16, torch.float32):
+    kind = lead.dtype if x is not None or x_out is not None else b16
+    if kind is not b16 and kind is not f32:
         raise TypeError(f"{where}: a stream of {kind}")
-    cap = 0
-    if x is not None:
-        want(where, "x", x, kind, shape)
-    if y is not None:
-        want(where, "y", y, torch.bfloat16, shape)
-    if y_sorted is not None:
-        want(where, "y_sorted", y_sorted, torch.bfloat16, (None, d))
-        cap = y_sorted.shape[0]
-    for name, t, dtype, size in (("pair_offsets", pair_offsets, torch.int32, T + 1),
-                                 ("pair_to_sorted", pair_to_sorted, torch.int32, cap),
-                                 ("pair_weight", pair_weight, torch.float32, cap),
-                                 ("w_post", w_post, torch.float32, d), ("w_pre", w_pre, torch.float32, d),
-                                 ("n_rows", n_rows, torch.int32, 1), ("q_scale", q_scale, torch.float32, T)):
-        if t is not None:
-            want(where, name, t, dtype, (size,))
-    for name, t, dtype in (("shared_y", shared_y, torch.bfloat16), ("x_out", x_out, kind),
-                           ("n_out", n_out, torch.bfloat16), ("q_out", q_out, torch.int8)):
-        if t is not None:
-            want(where, name, t, dtype, shape)
-    gates = 0
-    if gate is not None:
-        want(where, "gate", gate, torch.bfloat16, (None, d))
-        gates = gate.shape[0]
-    if seq_offsets is not None:
-        want(where, "seq_offsets", seq_offsets, torch.int32, (gates + 1,))
-    tensors = (x, y, y_sorted, pair_offsets, pair_to_sorted, pair_weight, shared_y, w_post, w_pre, gate,
-               seq_offsets, n_rows, x_out, n_out, q_out, q_scale)
-    args = NormArgsC(T, d, TYPE_F32 if kind == torch.float32 else TYPE_BF16, gates, cap, eps, residual_scale, 0,
-                     *[address(t) for t in tensors])
-    return args, (lead, *tensors)
+    cap = 0 if y_sorted is None else y_sorted.shape[0]
+    gates = 0 if gate is None else gate.shape[0]
+    tensors, addresses = [], []
+
+    # (a call's host time is these checks: what is as it should be is compared once, the rest named by want())
+    def take(name, t, dtype, size):
+        if t is None:
+            addresses.append(None)
+            return
+        if t.dtype is not dtype or t.shape != size or not t.is_contiguous():
+            want(where, name, t, dtype, size)
+        tensors.append(t)
+        addresses.append(t.data_ptr() or 256)
+    take("x", x, kind, shape)
+    take("y", y, b16, shape)
+    take("y_sorted", y_sorted, b16, (cap, d))
+    take("pair_offsets", pair_offsets, i32, (T + 1,))
+    take("pair_to_sorted", pair_to_sorted, i32, (cap,))
+    take("pair_weight", pair_weight, f32, (cap,))
+    take("shared_y", shared_y, b16, shape)
+    take("w_post", w_post, f32, (d,))
+    take("w_pre", w_pre, f32, (d,))
+    take("gate", gate, b16, (gates, d))
+    take("seq_offsets", seq_offsets, i32, (gates + 1,))
+    take("n_rows", n_rows, i32, (1,))
+    take("x_out", x_out, kind, shape)
+    take("n_out", n_out, b16, shape)
+    take("q_out", q_out, torch.int8, shape)
+    take("q_scale", q_scale, f32, (T,))
+    args = NormArgsC(T, d, TYPE_F32 if kind is f32 else TYPE_BF16, gates, cap, eps, residual_scale, 0, *addresses)
+    return args, tensors
 
 
 def reflex_block_norm(*arrays, stream=None, **named):

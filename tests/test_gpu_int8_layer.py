@@ -334,11 +334,11 @@ def test_rows_past_32_bits(torch, lib):
         assert not y.any()
 
 
-def test_experts_past_32_bits(torch, lib):
-    """Gathered rows, then activations, from 2^31 bytes on."""
+@pytest.mark.parametrize("sizes", [[5, 0, 9], [70, 0, 90]])      # (few rows, and tiles)
+def test_gathered_rows_past_32_bits(torch, lib, sizes):
     T, d, f = 131072 + 40, 16384, 128
     rng = np.random.default_rng(1)
-    c = expert_case(torch, lib, 1, d, f, [5, 0, 9])
+    c = expert_case(torch, lib, 1, d, f, sizes)
     c["T"] = T
     at = np.array([0, 77, 131071, 131072, 131073, T - 1])
     q, s = quant_rows(torch, lib, bf16(torch, rng.normal(size=(len(at), d))))
@@ -349,7 +349,9 @@ def test_experts_past_32_bits(torch, lib):
     c["token"] = at[rng.integers(0, len(at), c["cap"])].astype(np.int32)
     y = run_experts(torch, lib, c)
     check_experts(dict(c, h=q, hs=s, token=np.searchsorted(at, c["token"])), y)      # (of the rows that are there)
-    del c["h"], c["hs"]
+
+
+def test_activations_past_32_bits(torch, lib):
     rows = 131072 + 100
     c = expert_case(torch, lib, 8, 128, 16384, [rows])
     y = run_experts(torch, lib, c)
