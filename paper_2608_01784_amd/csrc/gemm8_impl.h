@@ -73,7 +73,6 @@ constexpr int G8_XCDS = 8;
 constexpr int G8_BK = F8_BLOCK;                  // bytes of a slice's row
 constexpr int G8_CHUNKS = G8_BK / 16;
 constexpr int G8_OP_ROWS = 64 / G8_CHUNKS;       // rows of one wave's copy (1 KB)
-constexpr int G8_NJ = 4;                         // 32-row weight blocks per wave
 // M tiles of a strip of a plain product of integers: an XCD's 32 workgroups then have 8 x 4 tiles, whose rows and
 // weights it reads from L2 (all tiles of a strip start with the same K), where 32 M tiles of one N tile pass L2 by.
 // 8192^3 463 -> 440 us, 8192 x 8192 x 2048 136 -> 130, 4096^3 with fp32 results 66.7 -> 65.3 (strips of 4 and 16: 439 and
@@ -186,8 +185,8 @@ __device__ __forceinline__ uint32_t stage_at(uint32_t stage, int row, int chunk)
 // The staged 32 rows x (128 / sizeof(OUT)) columns to `out`: rows row_base .. below row_end, columns
 // col_base .. below N.  8 lanes a row, 16 bytes each, at any address that the elements allow (rows of
 // an odd N start anywhere; global stores need no alignment beyond that).
-// (STREAM: whole vectors that pass the caches by)
-template <class OUT, bool ANY_N, bool STREAM = false>
+// (STREAM: whole vectors that pass the caches by; HALF: the first half of the columns)
+template <class OUT, bool ANY_N, bool STREAM = false, bool HALF = false>
 __device__ __forceinline__ void store_staged(int row_base, int col_base, int row_end, int N, OUT* __restrict__ out,
                                              uint32_t stage) {
   constexpr int VEC = 16 / sizeof(OUT), COLS = 128 / sizeof(OUT);
@@ -226,7 +225,7 @@ __device__ __forceinline__ void store_staged(int row_base, int col_base, int row
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int row = row_base + (lane >> 3) + 8 * q;
-    if (row < row_end && col < N) {
+    if (row < row_end && col < N && (!HALF || (lane & 7) < 4)) {
       OUT* const to = out + static_cast<size_t>(row) * N + col;
       if constexpr (STREAM)
         __builtin_nontemporal_store(v[q], reinterpret_cast<u32x4_t*>(to));
@@ -241,11 +240,12 @@ __device__ __forceinline__ void store_staged(int row_base, int col_base, int row
 // A_SLOTS input-row and B_SLOTS weight slices, copied A_SLOTS - 1 and B_SLOTS - 1 steps ahead.  (Blocks of
 // 128 x 128 a wave read half as much LDS per product as eight waves' of 128 x 64, whose reads and copies
 // alone would take all of the LDS's rate.)
-template <int MI_, int A_SLOTS_, int B_SLOTS_>
+template <int MI_, int A_SLOTS_, int B_SLOTS_, int NJ_ = 4>
 struct Shape8 {
+  static constexpr int NJ = NJ_;      // 32-row weight blocks per wave
   static constexpr int MI = MI_, WM = 2, WN = 2, WAVES = 4, A_SLOTS = A_SLOTS_, B_SLOTS = B_SLOTS_;
   static constexpr int THREADS = 64 * WAVES;
-  static constexpr int BM = 32 * MI * WM, BROWS = 32 * G8_NJ * WN;      // pair and weight rows of a tile
+  static constexpr int BM = 32 * MI * WM, BROWS = 32 * NJ * WN;      // pair and weight rows of a tile
   static constexpr int A_BYTES = BM * G8_BK, B_BYTES = BROWS * G8_BK;   // one slice
   static constexpr int A_OPS = BM / G8_OP_ROWS / WAVES, B_OPS = BROWS / G8_OP_ROWS / WAVES;   // a wave's copies
   static constexpr int B_WROWS = BROWS / WAVES;                         // weight rows a wave copies
@@ -255,8 +255,8 @@ struct Shape8 {
   static constexpr int IN_FLIGHT = (B_SLOTS > A_SLOTS ? B_OPS : 0) + (A_SLOTS - 2) * (A_OPS + B_OPS);
   static_assert(A_SLOTS >= 2 && B_SLOTS >= A_SLOTS, "shape");
   static_assert(A_OPS * G8_OP_ROWS * WAVES == BM && B_OPS * G8_OP_ROWS * WAVES == BROWS, "whole copies");
-  static_assert(WAVES * (G8_STAGE + 512) <= B_BYTES && 8 * BM <= B_BYTES, "the epilogue's scratch fits a weight slot");
-  static_assert(BROWS == 2 * F8_BLOCK && B_WROWS == F8_BLOCK / 2, "UP: half of the waves copy gate rows, half up rows");
+  static_assert(WAVES * (G8_STAGE + (NJ > 2 ? 512 : 0)) <= B_BYTES && 8 * BM <= B_BYTES, "the epilogue's scratch fits a weight slot");
+  static_assert(B_WROWS % 16 == 0, "UP: half of the waves copy gate rows, half up rows");
   static_assert(4 * (REFLEX_MAX_EXPERTS + 1) <= LDS, "start-up scratch in the rings");
   static_assert(LDS <= 160 * 1024 && IN_FLIGHT < 64, "LDS and vmcnt range");
 };
@@ -281,9 +281,10 @@ struct Args8 {
 // has 32 bits, of which the upper half is kept for skipped copies).
 template <Codes CODES, Mode MODE, class S, bool BIG, class OUT>
 __device__ __forceinline__ void gemm8(const Args8& a) {
-  constexpr int MI = S::MI, A_OPS = S::A_OPS, B_OPS = S::B_OPS;
+  constexpr int MI = S::MI, NJ = S::NJ, A_OPS = S::A_OPS, B_OPS = S::B_OPS;
   constexpr bool WIDE = CODES == F8 && MODE == PLAIN && sizeof(OUT) == 4;       // fp32 results of e4m3 codes
   using Acc = typename std::conditional<CODES == I8, i32x16_t, f32x16_t>::type;
+  static_assert(CODES == I8 || S::BROWS == 2 * F8_BLOCK, "a tile of one scale of the weights");
   constexpr int BN = MODE == UP ? S::BROWS / 2 : S::BROWS;       // output columns of a tile
   extern __shared__ __attribute__((aligned(16))) uint8_t smem8[];
   uint8_t* const a_ring = smem8;
@@ -539,10 +540,10 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
   };
   // ---- multiply: pair blocks WM i + wm, weight blocks b_row[j] of the tile
   // (UP: two blocks of gate rows, then the matching two of up rows)
-  int b_row[G8_NJ];
+  int b_row[NJ];
 #pragma unroll
-  for (int j = 0; j < G8_NJ; ++j)
-    b_row[j] = MODE == UP ? (j / 2) * (S::BROWS / 2) + 64 * wn + 32 * (j % 2) : 128 * wn + 32 * j;
+  for (int j = 0; j < NJ; ++j)
+    b_row[j] = MODE == UP ? j / (NJ / 2) * (S::BROWS / 2) + 16 * NJ * wn + 32 * (j % (NJ / 2)) : 32 * NJ * wn + 32 * j;
   // ---- scales: source rows of this lane's row of each pair block, of this tile and of the next;
   // their bytes of the current group; the weights' bytes of all K (UP: gate and up rows).
   // I8: the rows' scales and those of the wave's 128 weight rows, two a lane (UP: a gate and an up row)
@@ -561,7 +562,7 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
     if constexpr (CODES == I8) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int n = min(MODE == UP ? t.n0 + 64 * wn + l : t.n0 + 128 * wn + 64 * j + l, N - 1);
+        const int n = min(MODE == UP ? t.n0 + 16 * NJ * wn + l % (16 * NJ) : t.n0 + 32 * NJ * wn + 64 * (j % (NJ / 2)) + l, N - 1);
         const bool second = MODE == UP && j == 1;
         w_next[j] = (t.expert == E ? (second ? a.ss1 : a.ss0) : (second ? a.s1 : a.s0) + static_cast<size_t>(t.expert) * N)[n];
       }
@@ -620,9 +621,9 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
   auto tile = [&](auto nb_c) {
     constexpr int NB = decltype(nb_c)::value;
     const int l = lane_here(), frow = l & 31, fsel = l >> 5, fx = (frow / 2) % G8_CHUNKS;
-    Acc acc[NB > 0 ? NB : 1][G8_NJ];
+    Acc acc[NB > 0 ? NB : 1][NJ];
     constexpr int UNITS = 2 * NB, LATE = NB > 1 ? 2 : 1;
-    i32x8_t af[2 + LATE], bf[2][G8_NJ];
+    i32x8_t af[2 + LATE], bf[2][NJ];
     uint32_t late_sx[LATE], late_sw[2];      // the late units' scales
     auto slot_of = [](int u) { return u >= UNITS - LATE ? 2 + u - (UNITS - LATE) : u % 2; };
     // (fresh: the first products of a tile add to nothing)
@@ -635,7 +636,7 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
 #pragma unroll
         for (int q = 0; q < 2; ++q)
 #pragma unroll
-          for (int j = 0; j < G8_NJ; ++j) {
+          for (int j = 0; j < NJ; ++j) {
             auto half = [q](const i32x8_t& v) {
               return q ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
             };
@@ -649,13 +650,13 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
           const bf16x8_t xb =
               widen8(af[slot_of(u)][2 * q], af[slot_of(u)][2 * q + 1], __uint_as_float((sx & 0xffu) << 23));
 #pragma unroll
-          for (int j = 0; j < G8_NJ; ++j)
+          for (int j = 0; j < NJ; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(bf[kk][j][2 * q], bf[kk][j][2 * q + 1], sws), xb,
                                                                 FRESH && q == 0 ? zero : acc[i][j], 0, 0, 0);
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < G8_NJ; ++j)
+        for (int j = 0; j < NJ; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
               bf[kk][j], af[slot_of(u)], FRESH ? zero : acc[i][j], 0, 0, 0, static_cast<int>(sw[MODE == UP ? j / 2 : 0]), 0,
               static_cast<int>(sx));
@@ -680,7 +681,7 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
 #pragma unroll
         for (int j = 0; j < B_OPS; ++j) copy_b(j, Bn, kb);
       } else {
-        constexpr int kMfmas = WIDE ? 4 * G8_NJ : (CODES == I8 ? 2 * G8_NJ : G8_NJ);      // of a unit
+        constexpr int kMfmas = WIDE ? 4 * NJ : (CODES == I8 ? 2 * NJ : NJ);      // of a unit
         const uint8_t* const As = a_ring + (s % S::A_SLOTS) * S::A_BYTES;
         const uint8_t* const Bs = b_ring + (s % S::B_SLOTS) * S::B_BYTES;
         auto read = [&](const uint8_t* row, int kk) {
@@ -711,12 +712,12 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
           done = until;
         };
 #pragma unroll
-        for (int j = 0; j < G8_NJ; ++j) read_b(0, j);
+        for (int j = 0; j < NJ; ++j) read_b(0, j);
         // (not the late units' yet: their registers hold the previous slice's)
         constexpr int AHEAD = UNITS - LATE < 2 ? UNITS - LATE : 2;
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) read_a(u);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * G8_NJ + 2 * AHEAD, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NJ + 2 * AHEAD, 0);
         if constexpr (!FIRST) {
 #pragma unroll
           for (int l = 0; l < LATE; ++l) {
@@ -731,8 +732,8 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
           int reads = 0;
           if (u < NB) {
 #pragma unroll
-            for (int j = 0; j < G8_NJ; ++j)
-              if (j >= G8_NJ * u / NB && j < G8_NJ * (u + 1) / NB) {
+            for (int j = 0; j < NJ; ++j)
+              if (j >= NJ * u / NB && j < NJ * (u + 1) / NB) {
                 read_b(1, j);
                 reads += 2;
               }
@@ -823,12 +824,13 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
       // by, which leaves those to the weights' stream (experts of 1024 / 8192 tokens, E = 64, 120 -> 112 and 453 -> 448 us;
       // the whole layer with its norm 157 -> 154 and 569 -> 567, E = 256 249 -> 246).
       if constexpr (NB > 0) {
-        const uint32_t mine = scratch + S::WAVES * G8_STAGE + wave * 512;
+        const uint32_t stage = scratch + wave * G8_STAGE;
+        const uint32_t mine = NJ > 2 ? scratch + S::WAVES * G8_STAGE + wave * 512 : stage;
         asm volatile("ds_write_b32 %0, %1\n\tds_write_b32 %0, %2 offset:256\n\ts_waitcnt lgkmcnt(0)" ::"v"(mine + 4 * el),
                      "v"(w_cur[0]), "v"(w_cur[1])
                      : "memory");
         auto columns = [&](int j, f32x4_t (&w)[4]) {      // the scales of the lane's columns in block j
-          const uint32_t at = mine + 128 * j + 16 * esel;
+          const uint32_t at = mine + (MODE == UP ? j / (NJ / 2) * 256 + j % (NJ / 2) * 128 : 128 * j) + 16 * esel;
           asm volatile(
               "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\t"
               "ds_read_b128 %3, %4 offset:96\n\ts_waitcnt lgkmcnt(0)"
@@ -837,15 +839,14 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
               : "memory");
         };
         // (UP: read again for every pair block, two gate and up blocks at a time, which leaves the activation registers)
-        f32x4_t sw[G8_NJ][4];
-        if constexpr (MODE != UP) {
+        f32x4_t sw[NJ][4];
+        if constexpr (MODE != UP || NJ == 2) {
 #pragma unroll
-          for (int j = 0; j < G8_NJ; ++j) columns(j, sw[j]);
+          for (int j = 0; j < NJ; ++j) columns(j, sw[j]);
         }
         uint32_t sxb[MI];
         rows_scales(sxb);
         OUT* const out = static_cast<OUT*>(a.out);
-        const uint32_t stage = scratch + wave * G8_STAGE;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           __builtin_amdgcn_sched_barrier(0);      // (one block's registers at a time)
@@ -854,21 +855,23 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
           auto value = [&](int j, int r) { return static_cast<float>(acc[i][j][r]) * (sx * sw[j][r / 4][r % 4]); };
           if constexpr (MODE == UP) {
 #pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
+            for (int jj = 0; jj < NJ / 2; ++jj) {
               __builtin_amdgcn_sched_barrier(0);
-              columns(jj, sw[jj]);
-              columns(jj + 2, sw[jj + 2]);
+              if constexpr (NJ > 2) {
+                columns(jj, sw[jj]);
+                columns(jj + NJ / 2, sw[jj + NJ / 2]);
+              }
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
-                auto act = [&](int r) { return silu_mul(value(jj, 4 * g + r), value(jj + 2, 4 * g + r)); };
+                auto act = [&](int r) { return silu_mul(value(jj, 4 * g + r), value(jj + NJ / 2, 4 * g + r)); };
                 lds_write64(stage_at(stage, erow, 4 * jj + g) + 8 * esel, pack_bf16x2(act(0), act(1)),
                             pack_bf16x2(act(2), act(3)));
               }
             }
-            store_staged<OUT, false, true>(rb, t.n0 + 64 * wn, t.row_end, N, out, stage);
+            store_staged<OUT, false, true, NJ == 2>(rb, t.n0 + 16 * NJ * wn, t.row_end, N, out, stage);
           } else {
 #pragma unroll
-            for (int j = 0; j < G8_NJ; j += sizeof(OUT) == 4 ? 1 : 2) {
+            for (int j = 0; j < NJ; j += sizeof(OUT) == 4 ? 1 : 2) {
               __builtin_amdgcn_sched_barrier(0);
               if constexpr (sizeof(OUT) == 4) {
 #pragma unroll
@@ -884,7 +887,7 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
                                 pack_bf16x2(value(j + jj, 4 * g), value(j + jj, 4 * g + 1)),
                                 pack_bf16x2(value(j + jj, 4 * g + 2), value(j + jj, 4 * g + 3)));
               }
-              store_staged<OUT, MODE == PLAIN, MODE == DOWN>(rb, t.n0 + 128 * wn + 32 * j, t.row_end, N, out, stage);
+              store_staged<OUT, MODE == PLAIN, MODE == DOWN>(rb, t.n0 + 32 * NJ * wn + 32 * j, t.row_end, N, out, stage);
             }
           }
         }
@@ -972,7 +975,7 @@ __device__ __forceinline__ void gemm8(const Args8& a) {
           const int rb = t.row0 + 32 * (S::WM * i + wm);
           const uint32_t stage = scratch + wave * G8_STAGE;
 #pragma unroll
-          for (int j = 0; j < G8_NJ; j += sizeof(OUT) == 4 ? 1 : 2) {
+          for (int j = 0; j < NJ; j += sizeof(OUT) == 4 ? 1 : 2) {
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (sizeof(OUT) == 4) {
               const f32x16_t& c = acc[i][j];
@@ -1196,6 +1199,10 @@ __global__ __launch_bounds__(64 * W) void int8_slim_kernel(Args8 a) {
 using Tall = Shape8<4, 2, 3>;       // 256 x 256, 160 KB of LDS, one workgroup per CU
 using Half = Shape8<2, 3, 3>;       // 128 x 256, 144 KB
 using Quarter = Shape8<1, 3, 4>;    // 64 x 256, 152 KB
+// of integers alone, with no more than one scale a row (a tile's weights need not be 256 rows): two workgroups per CU,
+// of which one multiplies or copies while the other is between tiles
+using Low = Shape8<1, 3, 3, 2>;     // 64 x 128, 72 KB
+using Square = Shape8<2, 2, 3, 2>;  // 128 x 128, 80 KB
 
 // Lets a kernel have `lds` bytes of LDS; set_on: a bit a device (the attribute is the device's own).
 int allow_lds(const void* kernel, size_t lds, std::atomic<uint64_t>& set_on) {
@@ -1237,7 +1244,7 @@ int launch_as(const Args8& a, hipStream_t s) {
   static std::atomic<uint64_t> set_on{0};
   const int rc = allow_lds(reinterpret_cast<const void*>(kernel), S::LDS, set_on);
   if (rc != REFLEX_OK) return rc;
-  const int grid = (device_cus() + G8_XCDS - 1) / G8_XCDS * G8_XCDS;      // one workgroup per CU
+  const int grid = (device_cus() + G8_XCDS - 1) / G8_XCDS * G8_XCDS * (S::LDS <= 80 * 1024 ? 2 : 1);      // all resident
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::THREADS), S::LDS, s, a);
   return launch_status();
 }
@@ -1264,9 +1271,19 @@ int launch_gemm8(const Args8& a, int rows, hipStream_t s) {
   // Half tiles too where whole ones would leave half of the CUs idle (1024 x 4096 x 2048 28.8 -> 20.0 us, 413 x 13071 x
   // 768 33.9 -> 21.3; a little beyond, 264 x 17745 x 1152, 140 tiles, 28.9)
   constexpr int BN = MODE == UP ? Tall::BROWS / 2 : Tall::BROWS;
-  const bool half = static_cast<long long>(std::max(a.E, 1)) * ((rows + Tall::BM - 1) / Tall::BM) * ((a.N + BN - 1) / BN) <=
-                    device_cus() / 2;
-  if (rows <= Quarter::BM) return launch_as<CODES, MODE, Quarter, false, OUT>(a, s);
+  const long long whole = static_cast<long long>(std::max(a.E, 1)) * ((rows + Tall::BM - 1) / Tall::BM) * ((a.N + BN - 1) / BN);
+  const bool half = whole <= device_cus() / 2;
+  // Integers, us, 64 x 128 twice a CU / 64 x 256 (F8's): 256 experts of 3 x 2048 x 512 and 1024 tokens 170 / 181, of 1024
+  // columns and 128 tokens 216 / 231, 64 experts and 128 tokens 86.8 / 91.8, 64 x 131072 x 2048 with fp32 results 59.9 / 62.5
+  // (rings of 2 and 4 slots: 176, 221, 88.6, 62.1; three workgroups with 2 and 2: 172 and 62).  128 x 128 twice a CU /
+  // 128 x 256: 1024 x 4096 x 2048, 64 whole tiles, 16.3 / 20.0; against those themselves 300 x 20000 x 1024, 158 of them,
+  // 14.9 / 18.5, 1024 x 10000 x 2048 (160) 30.4 / 32.7, but 1024 x 50257 x 2048 (788) 137 / 119.
+  if constexpr (CODES == I8) {
+    if (rows <= Low::BM) return launch_as<CODES, MODE, Low, false, OUT>(a, s);
+    if (rows > Half::BM && whole <= device_cus() * 3 / 4) return launch_as<CODES, MODE, Square, false, OUT>(a, s);
+  } else {
+    if (rows <= Quarter::BM) return launch_as<CODES, MODE, Quarter, false, OUT>(a, s);
+  }
   if (rows <= Half::BM || half) return launch_as<CODES, MODE, Half, false, OUT>(a, s);
   return launch_as<CODES, MODE, Tall, false, OUT>(a, s);
 }

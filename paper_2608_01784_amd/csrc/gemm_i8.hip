@@ -182,14 +182,15 @@ int launch_few(const Args8& a, const uint16_t* act, hipStream_t s) {
   return a.K < 8 * G8_BK ? launch_few_as<MODE, 4>(a, act, s) : launch_few_as<MODE, 8>(a, act, s);
 }
 
-// Whether experts of so many rows (when all are loaded alike) take these kernels.  Their weights' stream reaches 4.6 TB/s,
-// that of the tiles 4.5 to 4.8, but only with many tiles.  Both products and the rounding between, up to 8 experts a
-// token, us, tiles / here: 64 experts of 3 x 2048 x 1024, 1 token 30 / 16, 4 40 / 31, 16 80 / 67, 64 89 / 85, 128 91 / 92;
-// 256 of 512, 4 tokens 37 / 26, 32 90 / 89, 128 163 / 159, 256 171 / 175, 512 176 / 188; 256 of 1024 with up to 4, 32 tokens
-// 115 / 108, 64 165 / 183; 8 of 4096 with up to 2, 1 token 40 / 24, 96 63 / 53.
+// Whether experts of so many rows (when all are loaded alike) take these kernels: while their weights are a short stream.
+// Both products and the rounding between, up to 8 experts a token, us, tiles / here: 64 experts of 3 x 2048 x 1024, 1
+// token 27 / 16, 4 36 / 31, 16 73 / 67, 32 80 / 79, 64 85 / 86; 256 of 512, 8 tokens 42 / 40, 16 67 / 57, 32 82 / 89,
+// 128 149 / 159; 256 of 1024 with up to 4, 16 tokens 69 / 66, 32 102 / 108; 8 of 4096 with up to 2, 8 tokens 55 / 47, 96
+// 54 / 53; 33 of 640 with up to 4, 16 tokens 32 / 25, 200 42 / 41.
 bool few_rows(int likely, int E, int cap, int d, int f, int sh_rows) {
   const double bytes = 3.0 * d * f * std::max(std::min(E, cap), 1);
-  return likely <= 32 && sh_rows <= 128 && bytes <= 1e9 && likely * bytes <= 6.4e9;
+  // (room for many rows of few tokens: a workgroup for every tile that there may be would be too many)
+  return likely <= 32 && cap <= 64 * E && sh_rows <= 128 && bytes <= 4.5e8 && likely * bytes <= 3e9;
 }
 
 size_t act_bytes(int rows, int f) { return align_up(2 * static_cast<size_t>(rows) * f + 1); }

@@ -95,7 +95,8 @@ def test_counted_rows_of_strips_and_cut_rounds(torch, lib, used):
     (400, 512, 1024, [100] * 30 + [0, 128, 3, 65], 0, 128),
     (300, 1664, 1024, [200, 0, 513, 256, 1, 257, 900, 130], 500, 128),      # (tiles of 256 rows would be few)
     (400, 512, 512, [300] * 12 + [0, 0, 700], 100, 128),
-    (500, 1280, 640, [300] * 12 + [0, 0, 700, 257], 100, 256),
+    (500, 1280, 640, [300] * 12 + [0, 0, 700, 257], 100, 128),
+    (500, 2048, 896, [300] * 12 + [0, 0, 700, 257], 100, 256),
     (700, 1408, 1152, [256] * 9 + [513, 600, 1, 0, 511, 255, 129, 64], 64, 256),
     (900, 384, 128, [5000], 0, 128)])
 def test_experts_of_many_tiles(torch, lib, T, d, f, sizes, extra, kind):
@@ -126,3 +127,15 @@ def test_both_kernels_of_experts_give_the_same(torch, lib):
     few["h"], few["hs"], few["T"] = c["h"][:20].contiguous(), c["hs"][:20].contiguous(), 20
     assert launched(torch, lambda: run_experts(torch, lib, few)) == [("few", UP), ("few", DOWN)]
     assert torch.equal(run_experts(torch, lib, few)[:20], many[:20])
+
+
+def test_room_for_more_rows_than_tokens(torch, lib):
+    """A large pair capacity with few rows in use: a grid that goes by the rows there are."""
+    c = expert_case(torch, lib, 2, 128, 128, [3, 0, 1], 1 << 22)
+    y = torch.full((c["cap"], 128), 5.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(lib.reflex_swiglu_int8_workspace_size(c["cap"], 3, 128), dtype=torch.uint8, device="cuda")
+    args = (c["h"], c["hs"], torch.from_numpy(c["token"]).cuda(), torch.from_numpy(c["offsets"]).cuda(), c["w_gate"], c["w_up"],
+            c["w_down"], c["s_gate"], c["s_up"], c["s_down"], y, ws)
+    assert launched(torch, lambda: lib.reflex_grouped_swiglu_int8(*args)) == [(UP, 64), (DOWN, 64)]
+    assert (y[4:] == 5.0).all()
+    check_experts(dict(c, cap=4), host(y[:4]).astype(np.float64))
