@@ -590,7 +590,7 @@ int reflex_grouped_swiglu_int8(const int8_t* h, const float* h_scale, const int3
  * Errors: NULL args or a struct without x, y and y_sorted, without any output, or with some arrays
  *  of a group alone (pair arrays with y_sorted, q_scale with q_out; n_out or q_out without w_pre)
  *  (REFLEX_ERR_NULL); y together with y_sorted, w_post, gate or shared_y without an output of the
- *  block to apply to, unknown stream_type, eps not positive and finite, residual_scale not finite
+ *  block to apply to, unknown stream_type, eps not positive and finite, residual_scale not finite, reserved not 0
  *  (REFLEX_ERR_PARAM); sizes and alignment (REFLEX_ERR_SHAPE; all matrices and weights 16 bytes).
  */
 typedef struct {

@@ -899,7 +899,7 @@ size_t reflex_sizeof_norm_args(void) { return sizeof(reflex_norm_args); }
 static int check_norm(const reflex_norm_args* a, bool rows_given) {
   if (a == nullptr) return REFLEX_ERR_NULL;
   const bool wide = a->stream_type == REFLEX_TYPE_F32, pairs = a->y_sorted != nullptr;
-  if (!wide && a->stream_type != REFLEX_TYPE_BF16) return REFLEX_ERR_PARAM;
+  if ((!wide && a->stream_type != REFLEX_TYPE_BF16) || a->reserved != 0) return REFLEX_ERR_PARAM;
   if (!(a->eps > 0.0f) || !std::isfinite(a->eps) || !std::isfinite(a->residual_scale)) return REFLEX_ERR_PARAM;
   const bool any_pair = pairs || a->pair_offsets != nullptr || a->pair_to_sorted != nullptr || a->pair_weight != nullptr;
   const bool block = a->y != nullptr || pairs || rows_given;

@@ -2,6 +2,7 @@
 // integers (int8.h), on the i8 MFMA.
 //
 //  UP:    act[j, :] = quantize(SiLU(x_j W_gate[e]^T) * (x_j W_up[e]^T)),  x_j = h[sorted_token[j]]
+//         (integers: rounded to bf16; a row has one scale, so its codes wait for all of its columns)
 //  DOWN:  y[j, :]   = act[j, :] W_down[e]^T
 //  PLAIN: out[i, :] = x[i, :] W^T, any N, the first n_rows rows (gemm8_slim where there are few tiles)
 // Both operands are K-contiguous codes.  Rows of one expert are contiguous; each workgroup counts
@@ -15,7 +16,8 @@
 // are, at the rate of the unscaled instruction and with no vector instruction between the
 // products.  A lane multiplies the same input rows in every slice: it loads their bytes four
 // slices at once, a group ahead.  The weights' bytes of a whole tile lie in one register, a dword
-// a lane.
+// a lane.  Integers have one fp32 scale a row of either operand, which the epilogue multiplies the
+// sums by: a row's is loaded a tile ahead, a column's goes through LDS into registers.
 //
 // Precision: the f8f6f4 MFMA adds its 64 products with about 17 bits below the largest of them
 // (measured: 1.4e-5 relative in the 2-norm, whatever K is), far inside the rounding to bf16 or e4m3
@@ -24,7 +26,8 @@
 // results therefore widens the codes to bf16 (one instruction for two, scale included; e4m3 numbers times
 // powers of two are bf16 numbers, at the ends of the range with move_scales) and multiplies on
 // v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are fp32: a quarter of the rate,
-// unnoticed where the weights' stream bounds the product.
+// unnoticed where the weights' stream bounds the product.  v_mfma_i32_32x32x32_i8 adds integers exactly, so
+// results do not depend on the tile, and fp32 results cost no more than bf16 ones.
 //
 // Data movement: operands go from global memory straight into LDS (16 bytes a lane) through rings
 // of slices.  LDS rows are 128 bytes (8 chunks of 16) with chunk c of row r in slot
@@ -43,9 +46,10 @@
 // What bounds it, measured: many rows by the MFMAs (8192 x 8192 x 8192 2.3 PFLOP/s, where a large
 // library product of this type reaches 2.7) and, with a short K, by the tiles' stores, which come from all
 // workgroups at once and are not hidden (8192 x 8192 x 2048 2.0; 64 experts of 3 x 2048 x 1024 with 53000
-// rows 1.65); few rows by the weights' stream (48 rows of 131072 x 2048 6.2 TB/s for bf16 results, 4.8 for
+// rows 1.65); the same of integers (2.5, where a library product reaches 2.2, and 2.0 to 2.1; 1.5 with the scales, SiLU and a
+// launch that rounds rows); few rows by the weights' stream (48 rows of 131072 x 2048 6.2 TB/s for bf16 results, 4.8 for
 // fp32 ones; experts 3.5 to 4.5 TB/s, whose launches are short and start with two dependent
-// loads).  Letting every second workgroup start half a tile later, so that stores meet products of others, cost
+// loads; integers, two workgroups a CU, 4.2 to 5.2).  Letting every second workgroup start half a tile later, so that stores meet products of others, cost
 // its delay (490 -> 512 us).
 #pragma once
 

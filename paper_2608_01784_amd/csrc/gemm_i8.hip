@@ -1,7 +1,10 @@
 // SwiGLU experts and plain products on 8-bit integer rows and weights (int8.h): the launches of gemm8_impl.h.
 //
 // A row of the activation has one scale, so its codes wait for all of its columns: the up product leaves bf16 rows,
-// which quantize_i8_kernel rounds to 8 bits ahead of the down product.
+// which quantize_i8_kernel rounds to 8 bits ahead of the down product (53000 rows of 1024: 32 of 454 us; 26 rows an expert
+// on 256 experts of width 512: 5 of 170).  bf16 ahead of the rounding: half a bf16 step at a row's largest number is a
+// quarter of an 8-bit step, everywhere else less, against the half step that every code is off by; fp32 rows would be
+// twice the bytes.
 #include "gemm8_impl.h"
 
 namespace rfx {
@@ -16,7 +19,7 @@ const uint32_t* bits(const float* p) { return reinterpret_cast<const uint32_t*>(
 // has 32 rows x 32 columns of gate and of up (UP) or x 64 columns (DOWN), 128 KB of weights at K = 2048, and its waves take
 // every FEW_W-th slice of 128 of K each, straight from global memory into the MFMAs' registers, a slice ahead of the
 // products (two took the registers that hold a second workgroup, 31 -> 37 us for the 4 tokens below); their sums meet in
-// LDS.  DOWN reads the activation's bf16 rows and rounds them to 8 bits itself, a row's maximum over the waves first,
+// LDS.  The first weights are asked for ahead of what the rows wait for (31 -> 29 us).  DOWN reads the activation's bf16 rows and rounds them to 8 bits itself, a row's maximum over the waves first,
 // which saves a launch.  Sums of integers are exact, so the results are those of the tiles.
 
 // 16 codes of 32 bytes of bf16.
@@ -64,8 +67,7 @@ __global__ __launch_bounds__(64 * FEW_W) void int8_few_kernel(Args8 a, const uin
   // (rows past the last are the last one's again, and not stored)
   const int row = min(row0 + lane % 32, row_end - 1);
   int src = row;
-  if (MODE == UP) src = on ? row - a.sh_row0 : a.gather[row];
-  src = min(max(src, 0), a.x_rows - 1);
+  if (MODE == UP && !on) src = a.gather[row];
   const size_t e0 = on ? size_t(0) : static_cast<size_t>(e) * N;
   const uint8_t* w[2];
 #pragma unroll
@@ -74,8 +76,6 @@ __global__ __launch_bounds__(64 * FEW_W) void int8_few_kernel(Args8 a, const uin
     const uint8_t* const base = MODE == UP && j == 1 ? (on ? a.sw1 : a.w1) : (on ? a.sw0 : a.w0);
     w[j] = base + (e0 + n) * K + 32 * (lane / 32);
   }
-  const uint8_t* const x = a.x + static_cast<size_t>(src) * K + 32 * (lane / 32);
-  const uint16_t* const xr = act + static_cast<size_t>(src) * K + 32 * (lane / 32);
   // A slice: lane l has bytes 32 (l / 32) .. of each half of its rows' 128 (of both operands alike)
   struct Slice {
     i32x4_t w[2][4], x[4];
@@ -89,6 +89,16 @@ __global__ __launch_bounds__(64 * FEW_W) void int8_few_kernel(Args8 a, const uin
         f.w[j][q] =
             *reinterpret_cast<const i32x4_t*>(w[j] + static_cast<size_t>(k) * G8_BK + 64 * (q / 2) + 16 * (q % 2));
   };
+  // (an access waits for those before it: UP's weights are asked for behind the rows' numbers and ahead of the rows, DOWN's
+  // behind its first rows)
+  if constexpr (MODE == UP) {
+    if (wave < nk) load_weights(slice, wave);
+    __builtin_amdgcn_sched_barrier(0);
+    if (on) src -= a.sh_row0;
+  }
+  src = min(max(src, 0), a.x_rows - 1);
+  const uint8_t* const x = a.x + static_cast<size_t>(src) * K + 32 * (lane / 32);
+  const uint16_t* const xr = act + static_cast<size_t>(src) * K + 32 * (lane / 32);
   auto load_rows = [&](Slice& f, int k) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -101,18 +111,24 @@ __global__ __launch_bounds__(64 * FEW_W) void int8_few_kernel(Args8 a, const uin
       }
     }
   };
+  if (wave < nk) load_rows(slice, wave);
   uint32_t most = 0;
   if constexpr (MODE == DOWN) {
-    for (int k = wave; k < nk; k += FEW_W) {
-      Slice f;
-      load_rows(f, k);
+    __builtin_amdgcn_sched_barrier(0);
+    auto maximum = [&](const Slice& f) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) most = max(most, max(i8_amax8(f.r[q][0]), i8_amax8(f.r[q][1])));
+    };
+    if (wave < nk) {
+      load_weights(slice, wave);
+      __builtin_amdgcn_sched_barrier(0);
+      maximum(slice);
     }
-  }
-  if (wave < nk) {
-    load_weights(slice, wave);
-    load_rows(slice, wave);
+    for (int k = wave + FEW_W; k < nk; k += FEW_W) {
+      Slice f;
+      load_rows(f, k);
+      maximum(f);
+    }
   }
   float factor = 0.0f;
   if constexpr (MODE == DOWN) {
@@ -184,9 +200,9 @@ int launch_few(const Args8& a, const uint16_t* act, hipStream_t s) {
 
 // Whether experts of so many rows (when all are loaded alike) take these kernels: while their weights are a short stream.
 // Both products and the rounding between, up to 8 experts a token, us, tiles / here: 64 experts of 3 x 2048 x 1024, 1
-// token 27 / 16, 4 36 / 31, 16 73 / 67, 32 80 / 79, 64 85 / 86; 256 of 512, 8 tokens 42 / 40, 16 67 / 57, 32 82 / 89,
-// 128 149 / 159; 256 of 1024 with up to 4, 16 tokens 69 / 66, 32 102 / 108; 8 of 4096 with up to 2, 8 tokens 55 / 47, 96
-// 54 / 53; 33 of 640 with up to 4, 16 tokens 32 / 25, 200 42 / 41.
+// token 27 / 16, 4 36 / 29, 16 73 / 64, 32 80 / 75, 64 85 / 84; 256 of 512, 8 tokens 42 / 38, 16 67 / 56, 32 82 / 89,
+// 128 149 / 159; 256 of 1024 with up to 4, 16 tokens 69 / 66, 32 102 / 108; 8 of 4096 with up to 2, 8 tokens 55 / 46, 96
+// 54 / 53; 33 of 640 with up to 4, 16 tokens 32 / 23, 200 42 / 42.
 bool few_rows(int likely, int E, int cap, int d, int f, int sh_rows) {
   const double bytes = 3.0 * d * f * std::max(std::min(E, cap), 1);
   // (room for many rows of few tokens: a workgroup for every tile that there may be would be too many)

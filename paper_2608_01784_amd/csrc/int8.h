@@ -9,7 +9,7 @@
 
 namespace rfx {
 
-constexpr uint32_t I8_LEAST = 0x0d800000u;      // 2^-100: s, 127 / a and s t's inverse stay normal numbers
+constexpr uint32_t I8_LEAST = 0x0d800000u;      // 2^-100: s and 127 / a are normal numbers
 constexpr uint32_t I8_INF = 0x7f800000u;
 
 // A product and a sum rounded to fp32 by themselves (the compiler would join them to one rounding otherwise).

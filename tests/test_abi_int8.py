@@ -92,7 +92,7 @@ PAIRS = dict(y_sorted=FAKE, pair_offsets=FAKE, pair_to_sorted=FAKE, pair_weight=
     (NULL, {**PAIRS, "pair_offsets": None}), (NULL, {**PAIRS, "pair_to_sorted": None}), (NULL, {**PAIRS, "y_sorted": None}),
     (NULL, {**PAIRS, "pair_weight": None}),
     (PARAM, {**PAIRS, "y": FAKE}), (PARAM, dict(y=FAKE, shared_y=FAKE)), (PARAM, dict(w_post=FAKE)),
-    (PARAM, dict(gate=FAKE, gate_rows=1)), (PARAM, dict(stream_type=2)), (PARAM, dict(stream_type=-1)), (PARAM, dict(eps=0.0)),
+    (PARAM, dict(gate=FAKE, gate_rows=1)), (PARAM, dict(stream_type=2)), (PARAM, dict(stream_type=-1)), (PARAM, dict(eps=0.0)), (PARAM, dict(reserved=1)),
     (PARAM, dict(eps=-1e-6)), (PARAM, dict(eps=float("nan"))), (PARAM, dict(eps=float("inf"))),
     (PARAM, dict(residual_scale=float("inf"))), (PARAM, dict(residual_scale=float("nan"))),
     (SHAPE, dict(T=-1)), (SHAPE, dict(T=MAX_T + 1)), (SHAPE, dict(d=192)), (SHAPE, dict(d=0)), (SHAPE, dict(d=MAX_D + 128)),
