@@ -80,7 +80,9 @@ def inside(got, ref, tol, rounding=2.0 ** -8):
 @pytest.mark.parametrize("T, d, E, f, fs, k", [
     (1, 128, 4, 128, 0, 2), (1, 256, 8, 128, 128, 8), (7, 384, 3, 256, 0, 1), (16, 256, 8, 128, 128, 2),
     (33, 512, 8, 256, 0, 3), (65, 256, 8, 128, 128, 2), (100, 256, 8, 128, 256, 2), (150, 640, 5, 384, 128, 5),
-    (300, 256, 2, 256, 256, 1), (40, 128, 64, 128, 128, 8), (520, 256, 4, 128, 0, 4)])
+    (300, 256, 2, 256, 256, 1), (40, 128, 64, 128, 128, 8), (520, 256, 4, 128, 0, 4),
+    (150, 256, 64, 128, 128, 2),       # (its rows in the tiles of the routed ones)
+    (5000, 256, 4, 128, 1280, 1)])     # (a shared expert of whole tiles)
 def test_layer(torch, lib, T, d, E, f, fs, k):
     from paper_2608_01784_amd.layer import MoELayerInt8
     rng = np.random.default_rng([T, d, E])
