@@ -349,6 +349,8 @@ def address(t):
 
 def want(where, name, t, dtypes, shape):
     """t: a dense tensor of one of `dtypes` and of `shape` (None: any size there)."""
+    if t.dtype is dtypes and t.shape == shape and t.is_contiguous():      # (most calls: a call's host time is its checks)
+        return
     if t.dtype not in (dtypes if isinstance(dtypes, tuple) else (dtypes,)):
         raise TypeError(f"{where}: {name} has element type {t.dtype}, not {dtypes}")
     have = t.shape
@@ -516,7 +518,7 @@ def reflex_quantize_int8(x, q, scale, rows=None, n_rows=None, stream=None):
     import torch
     where = "reflex_quantize_int8"
     M, K = q.shape
-    want(where, "x", x, torch.bfloat16, (None, K))
+    want(where, "x", x, torch.bfloat16, (x.shape[0], K))
     want(where, "q", q, torch.int8, (M, K))
     want(where, "scale", scale, torch.float32, (M,))
     if rows is not None:

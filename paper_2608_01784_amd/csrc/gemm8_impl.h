@@ -284,7 +284,7 @@ struct Args8 {
 // BIG: x of 2^31 bytes or more, addressed with 64-bit pointers (a buffer resource's byte offset
 // has 32 bits, of which the upper half is kept for skipped copies).
 template <Codes CODES, Mode MODE, class S, bool BIG, class OUT>
-__device__ __forceinline__ void gemm8(const Args8& a) {
+__device__ __forceinline__ void gemm8(Args8 a) {
   constexpr int MI = S::MI, NJ = S::NJ, A_OPS = S::A_OPS, B_OPS = S::B_OPS;
   constexpr bool WIDE = CODES == F8 && MODE == PLAIN && sizeof(OUT) == 4;       // fp32 results of e4m3 codes
   using Acc = typename std::conditional<CODES == I8, i32x16_t, f32x16_t>::type;
@@ -1056,7 +1056,7 @@ constexpr int SLIM_AHEAD = 2;
 constexpr int SLIM_PITCH = 65;      // floats between an accumulator's registers in LDS: no bank conflicts either way
 
 template <Codes CODES, int MI, int NJ, int W, class OUT>
-__device__ __forceinline__ void gemm8_slim(const Args8& a) {
+__device__ __forceinline__ void gemm8_slim(Args8 a) {
   constexpr bool WIDE = CODES == F8 && sizeof(OUT) == 4;
   using Acc = typename std::conditional<CODES == I8, i32x16_t, f32x16_t>::type;
   using Sum = typename std::conditional<CODES == I8, int, float>::type;
