@@ -537,8 +537,8 @@ int reflex_quantize_int8_weight(const uint16_t* w, int E, int N, int K, int8_t* 
 /*
  * out[i, n] = (sum_k x[i, k] w[n, k]) (x_scale[i] w_scale[n]): the sum of the codes' products is
  * exact, on the matrix cores; it, the product of the scales and the result are rounded to fp32
- * (off by at most 3 2^-24 of itself), for bf16 results then to bf16.  Rows from n_rows[0] on
- * (n_rows NULL: M) are left as they were.
+ * (off by at most 3 2^-24 of itself while the scales' product is a normal fp32 number), for bf16
+ * results then to bf16.  Rows from n_rows[0] on (n_rows NULL: M) are left as they were.
  *  x [M, K], x_scale [M];  w [N, K], w_scale [N];  out [M, N] dense (16-byte aligned), out_type
  *  REFLEX_TYPE_*
  * Errors: NULL pointers; sizes (REFLEX_ERR_SHAPE); unknown out_type (REFLEX_ERR_PARAM).
