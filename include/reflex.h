@@ -578,7 +578,7 @@ int reflex_grouped_swiglu_int8(const int8_t* h, const float* h_scale, const int3
  * with r(v) = 1 / sqrt(mean of v^2 + eps).  x NULL: no first term; w_post NULL: y_i as it is;
  * gate NULL: 1; w_pre NULL: no n (then n_out and q_out are NULL).  Products from the left, each
  * operation rounded to fp32 (the experts' rows by fused multiply-adds); mean and root are taken in
- * fp64 and r rounded to fp32, so results do not depend on how a row is split.
+ * fp64 and r rounded to fp32.
  *  x, x_out [T, d] of stream_type (REFLEX_TYPE_*);  y, shared_y, n_out [T, d] bf16;  w_post, w_pre
  *  [d] fp32;  y_sorted [pair_capacity, d] bf16 with pair_offsets [T+1], pair_to_sorted and
  *  pair_weight [pair_capacity] as in reflex_combine;  q_out [T, d], q_scale [T]

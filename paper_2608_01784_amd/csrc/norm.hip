@@ -5,9 +5,12 @@
 //   u = residual_scale x + gate (y r(y) w_post), rounded to the stream's type;  r(v) = 1 / sqrt(mean v^2 + eps)
 //   n = bf16(u r(u) w_pre);  codes and scale of n (int8.h)
 // One pass: W waves hold a row in registers, 16 numbers a lane, from the loads to the codes, and the weights over all
-// the rows that a workgroup takes.  Sums of squares are
-// taken in fp64 (a square of fp32 is exact there), so r is the rounded quotient whatever the order, and each product and sum
-// is rounded to fp32 by itself: results do not depend on W, and are those of the formulas, operation by operation, except for the experts' rows, which are added with fused multiply-adds in rank order as the combine does.
+// the rows that a workgroup takes.  Sums of squares are taken in fp64 (a square of fp32 is exact there), so r is the
+// rounded quotient in whatever order they are added (but for a row in some 10^8, next to a border), and each product and
+// sum is rounded to fp32 by itself: results are those of the formulas, operation by operation, except for the experts'
+// rows, which are added with fused multiply-adds in rank order as the combine does.  n is the norm of the stream as it is
+// stored, so that a later call on x_out gives the same, and the codes are those of the bf16 n, so that the router and the
+// experts read one input: that rounding is a quarter of a code's step at the row's largest number and less elsewhere.
 //
 // Bound by HBM.  16384 rows of 2048, bf16 stream, a gate for each sequence and both norms, 302 MB: 59 us or 5.1 TB/s,
 // what a large copy moves; 8192 tokens of 1 to 12 experts' rows with a shared one, 352 MB: 68 us.  What that took: 16
