@@ -189,7 +189,7 @@ __device__ __forceinline__ uint32_t stage_at(uint32_t stage, int row, int chunk)
 // The staged 32 rows x (128 / sizeof(OUT)) columns to `out`: rows row_base .. below row_end, columns
 // col_base .. below N.  8 lanes a row, 16 bytes each, at any address that the elements allow (rows of
 // an odd N start anywhere; global stores need no alignment beyond that).
-// (STREAM: whole vectors that pass the caches by; HALF: the first half of the columns)
+// (STREAM: whole vectors pass the caches by where rows are of whole ones; HALF: the first half of the columns)
 template <class OUT, bool ANY_N, bool STREAM = false, bool HALF = false>
 __device__ __forceinline__ void store_staged(int row_base, int col_base, int row_end, int N, OUT* __restrict__ out,
                                              uint32_t stage) {
@@ -231,7 +231,7 @@ __device__ __forceinline__ void store_staged(int row_base, int col_base, int row
     const int row = row_base + (lane >> 3) + 8 * q;
     if (row < row_end && col < N && (!HALF || (lane & 7) < 4)) {
       OUT* const to = out + static_cast<size_t>(row) * N + col;
-      if constexpr (STREAM)
+      if (STREAM && (!ANY_N || N % VEC == 0))
         __builtin_nontemporal_store(v[q], reinterpret_cast<u32x4_t*>(to));
       else
         __builtin_memcpy(to, &v[q], 16);
@@ -826,7 +826,9 @@ __device__ __forceinline__ void gemm8(Args8 a) {
       // The wave's column scales, through LDS into each lane's 4 x 16 columns; then a pair block at a time: the sums
       // times both scales (UP: the activation of gate and up), staged and stored as below.  Experts' rows pass the caches
       // by, which leaves those to the weights' stream (experts of 1024 / 8192 tokens, E = 64, 120 -> 112 and 453 -> 448 us;
-      // the whole layer with its norm 157 -> 154 and 569 -> 567, E = 256 249 -> 246).
+      // the whole layer with its norm 157 -> 154 and 569 -> 567, E = 256 249 -> 246), and so do plain products of small tiles
+      // (64 x 131072 x 2048 with fp32 results 60 -> 56 us, with the sampler after it 82.6 -> 81.8; 1024 x 4096 x 2048 17.7 ->
+      // 15.8; but 8192 x 8192 x 2048 130 and 131, 4096^3 66 and 69).
       if constexpr (NB > 0) {
         const uint32_t stage = scratch + wave * G8_STAGE;
         const uint32_t mine = NJ > 2 ? scratch + S::WAVES * G8_STAGE + wave * 512 : stage;
@@ -891,7 +893,7 @@ __device__ __forceinline__ void gemm8(Args8 a) {
                                 pack_bf16x2(value(j + jj, 4 * g), value(j + jj, 4 * g + 1)),
                                 pack_bf16x2(value(j + jj, 4 * g + 2), value(j + jj, 4 * g + 3)));
               }
-              store_staged<OUT, MODE == PLAIN, MODE == DOWN>(rb, t.n0 + 32 * NJ * wn + 32 * j, t.row_end, N, out, stage);
+              store_staged<OUT, MODE == PLAIN, MODE == DOWN || MI < 4>(rb, t.n0 + 32 * NJ * wn + 32 * j, t.row_end, N, out, stage);
             }
           }
         }
