@@ -228,6 +228,45 @@ def test_stack(torch, wide, T, fs):
     step(after=after)
 
 
+@pytest.mark.parametrize("T, fs", [(8, 128), (70, 0), (70, 128), (300, 256)])
+def test_join_over_the_layers_own_input(torch, T, fs):
+    """One norm for every layer: the join writes the rows that the layer has read."""
+    from paper_2608_01784_amd.layer import BlockNorm, MoELayerInt8
+    rng = np.random.default_rng([T, fs])
+    lay = MoELayerInt8(T, 256, random_weights(torch, 8, 256, 128, fs, 5), P(3), uniform_k=3)
+    w = [torch.from_numpy((1 + 0.2 * rng.normal(size=256)).astype(np.float32)).cuda() for _ in range(2)]
+    x = bf16(torch, rng.normal(size=(T, 256)))
+    a, b = x.clone(), x.clone()
+    one, turns = BlockNorm(T, 256, *w, eps=1e-5), [BlockNorm(T, 256, *w, eps=1e-5) for _ in range(2)]
+    one.start(a)
+    turns[0].start(b)
+    for i in range(4):
+        lay.forward(one.n, h_q=one.q, h_scale=one.scale, join=one.arrays(a))
+        now, then = turns[i % 2], turns[(i + 1) % 2]
+        lay.forward(now.n, h_q=now.q, h_scale=now.scale, join=then.arrays(b))
+        assert torch.equal(a, b) and torch.equal(one.n, then.n) and torch.equal(one.q, then.q) and torch.equal(one.scale, then.scale)
+
+
+@pytest.mark.parametrize("used", [0, 1, 40, 69, 70, 200])
+def test_join_of_counted_rows(torch, used):
+    """Rows behind the count keep their stream and their input."""
+    fill, step, results, (x, gate, seq) = stack_case(torch, L=1)
+    from paper_2608_01784_amd.layer import BlockNorm, MoELayerInt8
+    T = 70
+    lay = MoELayerInt8(T, 256, random_weights(torch, 8, 256, 128, 128, 6), P(3), uniform_k=3)
+    fill(0)
+    one = torch.ones(256, device="cuda")
+    norm, full = (BlockNorm(T, 256, one, one, eps=1e-5) for _ in range(2))
+    norm.start(x)
+    h, q, s, keep = norm.n.clone(), norm.q.clone(), norm.scale.clone(), x.clone()
+    want = x.clone()
+    lay.forward(h, h_q=q, h_scale=s, join=full.arrays(want, gate, seq))
+    lay.forward(h, h_q=q, h_scale=s, join=norm.arrays(x, gate, seq, torch.tensor([used], dtype=torch.int32, device="cuda")))
+    n = min(used, T)
+    for got, all_, before in ((x, want, keep), (norm.n, full.n, h), (norm.q, full.q, q), (norm.scale, full.scale, s)):
+        assert torch.equal(got[:n], all_[:n]) and torch.equal(got[n:], before[n:])
+
+
 def test_captured_stack(torch):
     fill, step, results, _ = stack_case(torch)
     want = []
