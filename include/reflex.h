@@ -282,7 +282,8 @@ int reflex_permute(const int32_t* pair_offsets, const int32_t* pair_expert, cons
  *   for each row j of expert e, x = h[sorted_token[j]],
  *   y_sorted[j] = W_down[e] (SiLU(W_gate[e] x) * (W_up[e] x)).
  * Both projections run on bf16 MFMA with fp32 accumulation; the activation
- * SiLU(g)*u is rounded to bf16 once, y once.
+ * SiLU(g)*u is rounded to bf16 once, y once.  SiLU may be taken as 0 for g below -87, where its
+ * magnitude is less than 2^-119.
  *  h        [T, d] bf16;  w_gate, w_up [E, f, d] bf16;  w_down [E, d, f] bf16
  *  y_sorted [pair_capacity, d] bf16 output (rows >= expert_offsets[E] untouched)
  *  ws       scratch of >= reflex_swiglu_workspace_size(pair_capacity, E, f)
@@ -472,9 +473,10 @@ int reflex_matmul_fp8(const uint8_t* x, const uint8_t* x_scale, const uint8_t* w
  * sorted_token[j] of h:  g = W_gate[e] x, u = W_up[e] x, SiLU(g) * u rounded to an 8-bit row
  * (as reflex_quantize_fp8 does, from fp32), y_sorted[j] = W_down[e] of it, rounded to bf16
  * once.  All three products are those of reflex_matmul_fp8 with bf16 results ahead of the
- * rounding (8-bit instruction, fp32 sums); SiLU is within (|g| + 4) 2^-22 of itself.  A value
- * that such an error takes across a border between two codes has the other one, a step away, and
- * a block's largest across a border between two scales moves the block's.
+ * rounding (8-bit instruction, fp32 sums); SiLU is within (|g| + 4) 2^-22 of itself for g from
+ * -87 on; below, where its magnitude is less than 2^-119, it may be taken as 0.  A value that an
+ * error takes across a border between two codes has the other one, a step away, and a block's
+ * largest across a border between two scales moves the block's.
  *  h [T, d], h_scale;  w_gate, w_up [E, f, d], w_down [E, d, f] with s_gate, s_up, s_down;
  *  sorted_token, expert_offsets, pair_capacity, y_sorted as in reflex_grouped_swiglu
  *  ws  scratch of >= reflex_swiglu_fp8_workspace_size(pair_capacity, E, f)
@@ -551,8 +553,9 @@ int reflex_matmul_int8(const int8_t* x, const float* x_scale, const int8_t* w, c
  * reflex_grouped_swiglu on 8-bit integers.  For row j of expert e, x the row sorted_token[j] of
  * h:  g = W_gate[e] x and u = W_up[e] x as fp32 results of reflex_matmul_int8, SiLU(g) * u rounded
  * to bf16, that row rounded to 8 bits as reflex_quantize_int8 does, y_sorted[j] = W_down[e] of it
- * as a bf16 result of reflex_matmul_int8.  SiLU is within (|g| + 4) 2^-22 of itself; a value that
- * this or a rounding takes across a border between two codes has the other one, a step away.
+ * as a bf16 result of reflex_matmul_int8.  SiLU is within (|g| + 4) 2^-22 of itself for g from
+ * -87 on; below, where its magnitude is less than 2^-119, it may be taken as 0.  A value that this
+ * or a rounding takes across a border between two codes has the other one, a step away.
  *  h [T, d], h_scale [T];  w_gate, w_up [E, f, d], w_down [E, d, f] with s_gate, s_up [E, f],
  *  s_down [E, d];  sorted_token, expert_offsets, pair_capacity, y_sorted as in
  *  reflex_grouped_swiglu

@@ -7,6 +7,8 @@ from __future__ import annotations
 
 import numpy as np
 
+from .int8 import FAR, steepest
+
 BLOCK = 128
 
 
@@ -101,17 +103,20 @@ def swiglu_rows(x, gate, up, down):
 
     A sum of n exact products in fp32 is off by at most n 2^-23 sum|terms| (each of the
     additions by one last place of a partial sum), and by dropped_bits() on the 8-bit MFMA.  The
-    activation inherits that (|SiLU'| <=
-    1.1, |SiLU(g)| <= |g|), and (|g| + 4) 2^-22 for the exponential and the division.  Rounded
+    activation inherits that (times the steepest SiLU there), and (|g| + 4) 2^-22 for the
+    exponential and the division.  Rounded
     to 8 bits the error vanishes, except that a value this near a border between two codes may
-    take the other one, a step away; near a block's scale border all of the block may."""
+    take the other one, a step away; near a block's scale border all of the block may.  A value of a
+    gate below FAR may be anything down to 0, and where it is its block's largest, the scale with it."""
     d, f = x.shape[1], gate.shape[0]
     g, ag = product(x, gate)
     u, au = product(x, up)
     eg, eu = d * 2.0 ** -23 * ag + dropped_bits(x, gate), d * 2.0 ** -23 * au + dropped_bits(x, up)
-    silu = g / (1.0 + np.exp(-g))
+    with np.errstate(over="ignore"):
+        sigma = 1.0 / (1.0 + np.exp(-g))
+    silu = g * sigma
     a = silu * u
-    ea = 1.1 * eg * (np.abs(u) + eu) + np.abs(silu) * eu + (np.abs(g) + 4.0) * 2.0 ** -22 * np.abs(a)
+    ea = steepest(g, eg, sigma) * eg * (np.abs(u) + eu) + np.abs(silu) * eu + (np.abs(g) + 4.0) * 2.0 ** -22 * np.abs(a)
     q, exps = quantize_rows(a)
     s = np.repeat(2.0 ** exps, BLOCK, axis=1)
     step = e4m3_step(a / s) * s
@@ -119,7 +124,10 @@ def swiglu_rows(x, gate, up, down):
     amax = np.abs(a).reshape(len(x), f // BLOCK, BLOCK).max(2)
     room = ea.reshape(len(x), f // BLOCK, BLOCK).max(2)
     border = (np.abs(amax - 448.0 * 2.0 ** exps) <= room) | (np.abs(amax - 448.0 * 2.0 ** (exps - 1)) <= room)
+    far = g - eg < FAR
+    border |= (far & (np.abs(a) >= np.repeat(amax - room, BLOCK, axis=1))).reshape(len(x), f // BLOCK, BLOCK).any(2)
     off = np.where(np.repeat(border, BLOCK, axis=1), 2.0 * step, np.where(near, step, 0.0))
+    off = np.where(far, 2.0 * step + np.abs(q), off)
     y, ay = product(q, down)
     moved = off @ np.abs(down).T
     return y, moved + f * 2.0 ** -23 * (ay + moved) + dropped_bits(np.abs(q) + off, down)

@@ -44,31 +44,45 @@ def product(x, xs, w, ws):
 PRODUCT_EPS = 3.1 * 2.0 ** -24      # the sum, the scales' product and the result rounded to fp32
 
 
+def steepest(g, eg, sigma):
+    """Largest |SiLU'| within eg of g, sigma the logistic function of g: |SiLU'(t)| <= sigma(t) (1 + |t|), at most 1.1
+    anywhere, and sigma(t) <= sigma(g) e^|t - g|."""
+    return np.minimum(1.1, sigma * np.exp(np.minimum(eg, 1.0)) * (1.0 + np.abs(g) + eg) + 1.1 * (eg > 1.0))
+
+
+FAR = -87.0      # below it SiLU, less than 2^-119 there, may be taken as 0 (the reciprocal of 1 + e^-g is no normal number)
+
+
 def swiglu_rows(x, xs, gate, up, down):
     """One expert (each weight a pair of codes and scales) on rows x, and how far a computation that
     follows the rounding points may be from it.
 
-    g and u are off by PRODUCT_EPS of themselves, the activation by that (|g SiLU'| <= 1.1 |g|) and
+    g and u are off by PRODUCT_EPS of themselves, the activation by that times the steepest SiLU there and
     (|g| + 4) 2^-22 of itself.  Rounded to bf16 the error vanishes, except next to a border between
     two numbers, where it is a step; then rounded to 8 bits the same, except that a row whose largest
-    number is itself in doubt may have another scale: then any value may move by a step."""
+    number is itself in doubt may have another scale: then any value may move by a step.  A value of a gate
+    below FAR may be anything down to 0."""
     g, u = product(x, xs, *gate), product(x, xs, *up)
     eg, eu = PRODUCT_EPS * np.abs(g), PRODUCT_EPS * np.abs(u)
     with np.errstate(over="ignore"):
-        silu = g / (1.0 + np.exp(-g))
+        sigma = 1.0 / (1.0 + np.exp(-g))
+    silu = g * sigma
     a = silu * u
-    ea = 1.1 * eg * (np.abs(u) + eu) + np.abs(silu) * eu + (np.abs(g) + 4.0) * 2.0 ** -22 * np.abs(a) + 2.0 ** -140
+    ea = steepest(g, eg, sigma) * eg * (np.abs(u) + eu) + np.abs(silu) * eu
+    ea += (np.abs(g) + 4.0) * 2.0 ** -22 * np.abs(a) + 2.0 ** -140
     step = bf16_step(a)
     doubt = np.abs(np.abs(a / step - np.floor(a / step)) - 0.5) <= ea / step
     b = bf16_round(a).astype(np.float64)
-    eb = np.where(doubt, step, 0.0)
+    far = g - eg < FAR
+    doubt |= far
+    eb = np.where(doubt, step, 0.0) + np.where(far, np.abs(b), 0.0)
     q, qs = quantize_rows(b)
     s = qs.astype(np.float64)[:, None]
     at = b / s
     near = np.abs(np.abs(at - np.floor(at)) - 0.5) <= eb / s + 127 * 2.0 ** -22
     top = np.abs(b).max(1, keepdims=True)
     moving = (doubt & (np.abs(b) >= top - 2.0 * step)).any(1, keepdims=True)
-    off = np.where(moving, 1.02 * s + eb, np.where(near, s, 0.0))
+    off = np.where(moving, 1.02 * s + eb, np.where(near, s + np.where(far, eb, 0.0), 0.0))
     y = product(q, qs, *down)
     w = np.abs(down[0].astype(np.float64)) * down[1].astype(np.float64)[:, None]
     return y, off @ w.T + PRODUCT_EPS * np.abs(y)

@@ -155,6 +155,9 @@ __device__ __forceinline__ void move_scales(uint32_t (&x)[MI], uint32_t& w) {
   }
 }
 
+// SiLU(g) u.  For g below -87 the reciprocal of 1 + e^-g is below the normal numbers, and v_rcp_f32 gives 0 for it: SiLU, of
+// magnitude less than 2^-119 there, is then 0.  (A second form for such gates, behind a test of each block's least, cost
+// 1 to 2 %: experts of 8192 tokens 443 -> 448 us in integers and 384 -> 388 in e4m3, of 1024 111 -> 114 and 110 -> 112.)
 __device__ __forceinline__ float silu_mul(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)) * u;
 }
