@@ -589,7 +589,8 @@ int reflex_grouped_swiglu_int8(const int8_t* h, const float* h_scale, const int3
  *            seq_offsets [gate_rows + 1], one for each sequence (rows past the last sequence have
  *            the last one's)
  *  n_rows    [1] int32 on the device or NULL: rows from n_rows[0] on are left as they were
- * x_out may be x; otherwise no output may share memory with an input or another output.
+ * x_out may be x and, of a bf16 stream, y or both at once (a row is read before it is written);
+ * otherwise no output may share memory with an input or another output.
  * Errors: NULL args or a struct without x, y and y_sorted, without any output, or with some arrays
  *  of a group alone (pair arrays with y_sorted, q_scale with q_out; n_out or q_out without w_pre)
  *  (REFLEX_ERR_NULL); y together with y_sorted, w_post, gate or shared_y without an output of the

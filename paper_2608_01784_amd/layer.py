@@ -360,7 +360,7 @@ class BlockNorm:
 
     def forward(self, x, y, gate=None, seq_offsets=None, n_rows=None, x_out=None, stream=None):
         """The block's output y (bf16 [T, d]) into the stream; returns the next block's input (None without a
-        norm before)."""
+        norm before).  x_out may be y's memory where the stream is bf16."""
         _lib.reflex_block_norm(y=y, stream=stream, **self.arrays(x, gate, seq_offsets, n_rows, x_out))
         return self.n
 
