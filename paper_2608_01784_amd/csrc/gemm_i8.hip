@@ -2,9 +2,10 @@
 //
 // A row of the activation has one scale, so its codes wait for all of its columns: the up product leaves bf16 rows,
 // which quantize_i8_kernel rounds to 8 bits ahead of the down product (53000 rows of 1024: 32 of 454 us; 26 rows an expert
-// on 256 experts of width 512: 5 of 170).  bf16 ahead of the rounding: half a bf16 step at a row's largest number is a
-// quarter of an 8-bit step, everywhere else less, against the half step that every code is off by; fp32 rows would be
-// twice the bytes.
+// on 256 experts of width 512: 5 of 170).  bf16 ahead of the rounding: it moves a number by up to a quarter to a half of an
+// 8-bit step where it is within a factor of two of the row's largest, by half as much for each factor of two below, beside
+// the half step that every code is off by; fp32 rows would be twice the bytes.  (The kernels for few rows save the launch:
+// there a workgroup reads a tile's whole rows anyway.)
 #include "gemm8_impl.h"
 
 namespace rfx {
@@ -19,7 +20,8 @@ const uint32_t* bits(const float* p) { return reinterpret_cast<const uint32_t*>(
 // has 32 rows x 32 columns of gate and of up (UP) or x 64 columns (DOWN), 128 KB of weights at K = 2048, and its waves take
 // every FEW_W-th slice of 128 of K each, straight from global memory into the MFMAs' registers, a slice ahead of the
 // products (two took the registers that hold a second workgroup, 31 -> 37 us for the 4 tokens below); their sums meet in
-// LDS.  The first weights are asked for ahead of what the rows wait for (31 -> 29 us).  DOWN reads the activation's bf16 rows and rounds them to 8 bits itself, a row's maximum over the waves first,
+// LDS.  The first weights are asked for ahead of what the rows wait for (31 -> 29 us).  DOWN reads the activation's bf16
+// rows and rounds them to 8 bits itself, a row's maximum over the waves first,
 // which saves a launch.  Sums of integers are exact, so the results are those of the tiles.
 
 // 16 codes of 32 bytes of bf16.
