@@ -49,8 +49,8 @@
 // rows 1.65); the same of integers (2.5, where a library product reaches 2.2, and 2.0 to 2.1; 1.5 with the scales, SiLU and a
 // launch that rounds rows); few rows by the weights' stream (48 rows of 131072 x 2048 6.2 TB/s for bf16 results, 4.8 for
 // fp32 ones; experts 3.5 to 4.5 TB/s, whose launches are short and start with two dependent
-// loads; integers, two workgroups a CU, 4.2 to 5.2).  Letting every second workgroup start half a tile later, so that stores meet products of others, cost
-// its delay (490 -> 512 us).
+// loads; integers, two workgroups a CU, 4.2 to 5.2).  Letting every second workgroup start half a tile later, so that
+// stores meet products of others, cost its delay (490 -> 512 us).
 #pragma once
 
 #include <algorithm>
@@ -1283,10 +1283,11 @@ int launch_gemm8(const Args8& a, int rows, hipStream_t s) {
   const long long whole = static_cast<long long>(std::max(a.E, 1)) * ((rows + Tall::BM - 1) / Tall::BM) * ((a.N + BN - 1) / BN);
   const bool half = whole <= device_cus() / 2;
   // Integers, us, 64 x 128 twice a CU / 64 x 256 (F8's): 256 experts of 3 x 2048 x 512 and 1024 tokens 170 / 181, of 1024
-  // columns and 128 tokens 216 / 231, 64 experts and 128 tokens 86.8 / 91.8, 64 x 131072 x 2048 with fp32 results 59.9 / 62.5
-  // (rings of 2 and 4 slots: 176, 221, 88.6, 62.1; three workgroups with 2 and 2: 172 and 62).  128 x 128 twice a CU /
-  // 128 x 256: 1024 x 4096 x 2048, 64 whole tiles, 16.3 / 20.0; against those themselves 300 x 20000 x 1024, 158 of them,
-  // 14.9 / 18.5, 1024 x 10000 x 2048 (160) 30.4 / 32.7, but 1024 x 50257 x 2048 (788) 137 / 119.
+  // columns and 128 tokens 216 / 231, 64 experts and 128 tokens 86.8 / 91.8, 64 x 131072 x 2048 with fp32 results 59.9 / 62.5,
+  // both before those results passed the caches by, 56 since (rings of 2 and 4 slots: 176, 221, 88.6, 62.1; three
+  // workgroups with 2 and 2: 172 and 62).  128 x 128 twice a CU / 128 x 256: 1024 x 4096 x 2048, 64 whole tiles, 16.3 / 20.0;
+  // against those themselves 300 x 20000 x 1024, 158 of them, 14.9 / 18.5, 1024 x 10000 x 2048 (160) 30.4 / 32.7, but 1024 x
+  // 50257 x 2048 (788) 137 / 119.
   if constexpr (CODES == I8) {
     if (rows <= Low::BM) return launch_as<CODES, MODE, Low, false, OUT>(a, s);
     if (rows > Half::BM && whole <= device_cus() * 3 / 4) return launch_as<CODES, MODE, Square, false, OUT>(a, s);

@@ -14,11 +14,15 @@
 // factor of two of the row's largest (half a bf16 step is 2^(k-8) from 2^k on, a code's step a / 127), by half as much for
 // each factor of two below, beside the half step that every code is off by.
 //
-// Bound by HBM.  16384 rows of 2048, bf16 stream, a gate for each sequence and both norms, 302 MB: 59 us or 5.1 TB/s,
-// what a large copy moves; 8192 tokens of 1 to 12 experts' rows with a shared one, 352 MB: 68 us.  What that took: 16
-// numbers a lane, not 32 (80 -> 75 us, joined rows 95 -> 82: more rows in flight), loads and stores that pass the caches
-// by (80 -> 70), all of a row's loads ahead of its first sum, and weights loaded once a workgroup (together 59).  fp64
-// sums cost nothing here (80 us with fp32 ones 76, before the rest).
+// Bound by HBM.  16384 rows of 2048, bf16 stream, a gate for each sequence and both norms, 302 MB: 56 to 62 us (cards
+// differ) or 4.9 to 5.4 TB/s, what a large copy moves; 8192 tokens of 1 to 12 experts' rows with a shared one, 352 MB: 67 us.
+// What that took: 16 numbers a lane, not 32 (80 -> 75 us, joined rows 95 -> 82: more rows in flight), loads and stores that
+// pass the caches by (80 -> 70), all of a row's loads ahead of its first sum, and weights loaded once a workgroup (together
+// 59).  The fp64 sums cost 5 % of the given rows, 62 us to 59 with fp32 ones on one card, and nothing of the joined ones (67).
+// Other widths, one gate, both norms, as many numbers, bf16 / fp32 stream, TB/s: given rows of 512 4.5 / 4.8, of 1024 5.4 /
+// 5.0, of 4096 5.2 / 5.0, of 8192 5.0 / 5.0, of 16384 4.6 / 4.5; 1 to 8 joined rows of 512 4.3 / 4.8, of 4096 5.2 / 5.1, of
+// 16384 4.6 / 4.6 (the instance for fp32 ones spills 8 registers).  Rows of 128 leave three quarters of a wave's lanes idle:
+// 1.5 / 2.2.
 #include "int8.h"
 
 namespace rfx {
